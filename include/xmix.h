@@ -45,7 +45,10 @@
  * (xmix_probe_score, xmix_sae_encode_topk and its stages); the writes
  * (xmix_steer_apply, xmix_sae_clamp_decode, xmix_router_write); readback
  * (xmix_readback_compact, or fused into the SAE merge with the _ring
- * variants).  Step graphs (xmix_graph_*) capture and replay such a
+ * variants).  At an attention hook (Fig. 2, `.submodule("attention.post")`)
+ * the rows come from the layer's attention over the batch's cached keys and
+ * values: xmix_qk_norm_rope, xmix_kv_append, xmix_paged_attention, in this
+ * order and before the reads.  Step graphs (xmix_graph_*) capture and replay such a
  * sequence.
  */
 #ifndef XMIX_H
@@ -66,14 +69,20 @@ typedef enum {
     XMIX_E_LAUNCH = 4        /* the HIP runtime rejected a launch */
 } xmix_status;
 
-typedef enum { XMIX_F32 = 0, XMIX_BF16 = 1 } xmix_dtype;
+/* XMIX_E4M3 (the OCP 8-bit float: 4 exponent bits, 3 of the fraction, largest
+ * value 448, no infinity) is a type of cached keys and values only. */
+typedef enum { XMIX_F32 = 0, XMIX_BF16 = 1, XMIX_E4M3 = 2 } xmix_dtype;
 
 enum { XMIX_PROBE_TOKEN = 0, XMIX_PROBE_MEAN = 1, XMIX_PROBE_LAST = 2 };
 
-/* Device error-word bits set by xmix_route_build. */
+/* Device error-word bits: the first two set by xmix_route_build, the others
+ * by xmix_kv_append and xmix_paged_attention. */
 enum {
     XMIX_ERR_REQUEST_RANGE = 1u,  /* a live token named a request id >= R_max */
-    XMIX_ERR_T_VALID = 2u         /* *T_valid was outside [0, T_max]; clamped */
+    XMIX_ERR_T_VALID = 2u,        /* *T_valid was outside [0, T_max]; clamped */
+    XMIX_ERR_KV_SLOT = 4u,  /* an appended token's position or page is not in the cache */
+    XMIX_ERR_KV_SPAN = 8u,  /* a request's span or key count is out of range */
+    XMIX_ERR_KV_PAGE = 16u  /* a page id that a request's keys need is out of range */
 };
 
 #define XMIX_MAX_APPS 32
@@ -556,6 +565,135 @@ xmix_status xmix_readback_compact(const void *const *seg_rows, const int32_t *se
                                   int32_t n_seg, const xmix_route *rt, int32_t app_bit,
                                   const int32_t *req_of_token, int32_t layer_id,
                                   int32_t app_id, const xmix_ring *ring, void *stream);
+
+/* ------------------------------------------- attention of a serving step
+ * The rows at an attention hook (Fig. 2, `.submodule("attention.post")`) are
+ * the outputs of the layer's attention heads for the tokens of the batch, over
+ * the keys and values that the batch's requests have cached (Sec. 2: a
+ * continuous batch mixes requests of any length).  Three calls make them from
+ * the projections' output, on the batch description of the hook step:
+ * xmix_qk_norm_rope, xmix_kv_append, xmix_paged_attention.
+ *
+ * Activations of heads are [T_max, n_heads, head_dim]: a token's heads are
+ * contiguous, and its row starts `stride` elements after the previous one's
+ * (stride >= n_heads * head_dim for outputs), so queries, keys and values can
+ * be parts of one projection's output.  Rows are 16-byte aligned: the pointer,
+ * and stride * element size, are multiples of 16. */
+
+/* Position rotation (host struct).  A head's first rot_dim values are rotated
+ * in pairs i < rot_dim / 2 by the angle position * inv_freq[i] (radians, both
+ * taken in fp64, so far positions keep their angle):
+ *   (a, b) -> (a cos - b sin, b cos + a sin)
+ * pairing XMIX_ROPE_HALF:  a = x[i], b = x[i + rot_dim / 2];
+ * pairing XMIX_ROPE_PAIRS: a = x[2 i], b = x[2 i + 1].
+ * inv_freq [rot_dim / 2] fp64, device, 16-byte aligned; rot_dim % 16 == 0,
+ * 16 <= rot_dim <= head_dim. */
+enum { XMIX_ROPE_HALF = 0, XMIX_ROPE_PAIRS = 1 };
+typedef struct {
+    const double *inv_freq;
+    int32_t rot_dim;
+    int32_t pairing;
+} xmix_rope;
+
+/* Paged cache of one layer's keys and values (host struct, device arrays,
+ * caller-owned):
+ *   k, v    [n_pages][n_kv][page_size][head_dim] of dtype dt, XMIX_BF16 or
+ *           XMIX_E4M3, 16-byte aligned
+ *   pages   [R_max][max_pages] int32: request r's position p lies in page
+ *           pages[r][p / page_size], slot p % page_size.  Entries past a
+ *           request's last position are not read; pages may be shared by
+ *           requests that read them (a common prefix).
+ *   k_scale, v_scale  [n_kv] fp32, XMIX_E4M3 only (NULL for XMIX_BF16): a
+ *           stored value x stands for x * scale of its head; positive, finite.
+ * page_size is a power of two from 16 to 4096, head_dim a multiple of 16 up to
+ * 256, max_pages * page_size < 2^31. */
+typedef struct {
+    void *k;
+    void *v;
+    const int32_t *pages;
+    const float *k_scale;
+    const float *v_scale;
+    int32_t n_pages, page_size, n_kv, head_dim, R_max, max_pages;
+    xmix_dtype dt;
+} xmix_kv_cache;
+
+/* Norm of every query and key head with the position rotation, in one pass:
+ * for each token t with pos_of_token[t] >= 0 and each head,
+ *   y = x * (mean(x^2) + eps)^(-1/2) * weight    (weight NULL: y = x)
+ *   out = round(rotate(y, pos_of_token[t]))      (rope NULL: no rotation)
+ * in fp32, rounded once to the storage type.  Rows of tokens with a negative
+ * position (padding), or at or past *T_valid, are not written.
+ * q [T_max, n_q, head_dim], k [T_max, n_kv, head_dim] of dtype `dt` (F32 or
+ * BF16) with row strides in elements; q_out, k_out likewise.  An output may be
+ * its own input (same pointer and stride); otherwise they do not overlap.
+ * k may be NULL with n_kv = 0 (queries alone, where xmix_kv_append rotates the
+ * keys).  q_weight, k_weight [head_dim] of dtype `dt`, 16-byte aligned.
+ * T_valid [1] int32, device; NULL: every row.
+ * Requires head_dim % 16 == 0, 16 <= head_dim <= 256, eps >= 0.
+ * Errors: XMIX_E_INVAL (null pointer, size, stride or alignment). */
+xmix_status xmix_qk_norm_rope(const void *q, int64_t q_stride, int32_t n_q, const void *k,
+                              int64_t k_stride, int32_t n_kv, xmix_dtype dt, int32_t head_dim,
+                              int32_t T_max, const int32_t *pos_of_token, const void *q_weight,
+                              const void *k_weight, float eps, const xmix_rope *rope, void *q_out,
+                              int64_t q_out_stride, void *k_out, int64_t k_out_stride,
+                              const int32_t *T_valid, void *stream);
+
+/* Append of a step's keys and values to the cache, the keys rotated on the
+ * way (rope NULL: stored as they are).  For each token t below *T_valid with
+ * req_of_token[t] >= 0 and pos_of_token[t] >= 0, each key and value head is
+ * stored at the token's slot as round(x), or with XMIX_E4M3 as x / scale of its
+ * head, held to [-448, 448] (NaN stays NaN) and rounded; the rotation and the
+ * division are in fp32.  No other slot is written.  A token whose request id is
+ * >= R_max, whose position is >= max_pages * page_size or whose page id is
+ * outside [0, n_pages) is not stored and sets XMIX_ERR_KV_SLOT.
+ * Two tokens of one batch must not name the same slot (what it then holds is
+ * some of either).
+ * k, v [T_max, n_kv, head_dim] of dtype `dt` (F32 or BF16), row strides in
+ * elements; T_valid [1] int32, device; NULL: every row.
+ * Errors: XMIX_E_INVAL (null pointer, size, stride or alignment). */
+xmix_status xmix_kv_append(const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                           xmix_dtype dt, int32_t T_max, const int32_t *req_of_token,
+                           const int32_t *pos_of_token, const xmix_rope *rope,
+                           const xmix_kv_cache *cache, uint32_t *err_word,
+                           const int32_t *T_valid, void *stream);
+
+/* Attention of the step's tokens over the pages of their requests.  Request r
+ * has the n = cu_seqlens[r+1] - cu_seqlens[r] tokens of its span (contiguous
+ * rows) and kv_len[r] cached keys, the last n of them those tokens' own: token
+ * i of the span is at position p = kv_len[r] - n + i and attends to the keys
+ * j <= p, with window > 0 also j > p - window.  For query head g, with key head
+ * g / (n_q / n_kv):
+ *   s_j = scale * (q . k_j),  lse = log sum_j exp(s_j),
+ *   out = sum_j exp(s_j - lse) v_j
+ * with q . k_j in exact bf16 products summed in fp32, the statistics in fp32,
+ * exp(s_j - max) rounded to bf16 where it multiplies v_j, and one rounding of
+ * out.  A masked key has no effect whatever its slots hold (NaN, infinities).
+ * A token without a key (p < 0) gets zeros and lse = -infinity.
+ * One call serves any mix of spans: one token per request (decode), a few
+ * (drafted tokens), chunks of a prompt.  The keys of a span are shared out in
+ * parts that depend on the lengths of the whole batch and are joined in a fixed
+ * order: equal calls give equal bits.
+ * q [T_max, n_q, head_dim] bf16, out likewise, row strides in elements;
+ * lse_out [n_q][T_max] fp32, or NULL.  Rows outside every span are not written.
+ * cu_seqlens [R_max + 1], kv_len [R_max] int32, device; max_q (host): no span
+ * is longer.  A span outside [0, T_max] or longer than max_q, or a key count
+ * outside [0, max_pages * page_size] of a request with tokens, sets
+ * XMIX_ERR_KV_SPAN and the request's rows are not written.  A page id outside
+ * [0, n_pages) sets XMIX_ERR_KV_PAGE and its keys are left out.
+ * Requires head_dim 64, 128 or 256, n_q % n_kv == 0, scale > 0 and finite,
+ * window >= 0, 1 <= max_q, R_max <= 4096.
+ * ws: 16-byte aligned device workspace of xmix_paged_attention_workspace
+ * bytes; nothing in it has to start at zero, and nothing is kept from call to
+ * call.  Calls that overlap in time need workspaces of their own.
+ * Errors: XMIX_E_INVAL (null pointer, size, stride or alignment),
+ * XMIX_E_UNSUPPORTED (head_dim, R_max), XMIX_E_WORKSPACE. */
+size_t xmix_paged_attention_workspace(int32_t T_max, int32_t n_q, int32_t max_q,
+                                      const xmix_kv_cache *cache);
+xmix_status xmix_paged_attention(const uint16_t *q, int64_t q_stride, int32_t n_q, int32_t T_max,
+                                 const int32_t *cu_seqlens, const int32_t *kv_len,
+                                 const xmix_kv_cache *cache, float scale, int32_t window,
+                                 int32_t max_q, uint16_t *out, int64_t out_stride, float *lse_out,
+                                 uint32_t *err_word, void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------ step graphs
  * A hook step captured once and replayed, with the kernel-node parameter

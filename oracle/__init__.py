@@ -48,7 +48,11 @@ def _load():
     lib.oracle_sae_encode.argtypes = [vp, i32, vp, i32, vp, vp, vp, i32, i32, vp, vp, vp, vp]
     lib.oracle_clamp_decode.argtypes = [vp, i32, i32, vp, i32, vp, vp, i32, vp, i32, vp, vp, i32, vp]
     lib.oracle_compact.argtypes = [vp, vp, i32, vp, i32, i32, vp, i32, i32, vp, i32, i32, vp]
-    for n in ("oracle_route", "oracle_route_gate", "oracle_route_trigger", "oracle_steer", "oracle_probe_token", "oracle_probe_mean", "oracle_probe_last",
+    f64 = ctypes.c_double
+    lib.oracle_norm_rope.argtypes = [vp, ctypes.c_int, i32, i32, i32, vp, vp, f64, vp, i32, i32, vp]
+    lib.oracle_attend.argtypes = [vp, i32, i32, i32, vp, vp, i32, vp, vp, vp, i32, i32, i32, i32, f64,
+                                  i32, vp, vp, vp, vp]
+    for n in ("oracle_norm_rope", "oracle_attend", "oracle_route", "oracle_route_gate", "oracle_route_trigger", "oracle_steer", "oracle_probe_token", "oracle_probe_mean", "oracle_probe_last",
               "oracle_sae_pre", "oracle_topk", "oracle_sae_encode", "oracle_clamp_decode",
               "oracle_compact"):
         getattr(lib, n).restype = None
@@ -274,3 +278,34 @@ def compact(segments, tok_mask, app_bit, req, layer_id, app_id, slots, head):
                            _p(_c(tok_mask, np.uint32)), T_max, int(app_bit), _p(_c(req, np.int32)),
                            int(layer_id), int(app_id), _p(out), cap, row_bytes, _p(hd))
     return out, int(hd[0])
+
+
+def norm_rope(x, pos, weight=None, eps=0.0, inv_freq=None, pairs=False):
+    """Heads x [T, n, hd] (bf16 bits or float32), normed by weight [hd] (None: not)
+    and rotated to their positions (inv_freq None: not), as unrounded float64;
+    rows of negative positions are NaN."""
+    bf16 = x.dtype == np.uint16
+    x, pos = np.ascontiguousarray(x), _c(pos, np.int32)
+    T, n, hd = x.shape
+    w = None if weight is None else np.ascontiguousarray(weight)
+    f = None if inv_freq is None else _c(inv_freq, np.float64)
+    out = np.full(x.shape, np.nan)
+    _load().oracle_norm_rope(_p(x), int(bf16), T, n, hd, _p(pos), _p(w), float(eps), _p(f),
+                             0 if f is None else 2 * f.size, int(pairs), _p(out))
+    return out
+
+
+def attend(q, cu, kv_len, k, v, pages, scale, window=0):
+    """Attention of q [T, n_q, hd] (bf16 bits) over widened pages k, v [n_pages, n_kv,
+    page_size, hd].  Returns out, lse [n_q, T], and the two bounds mag and big of
+    oracle_attend; rows outside every span are NaN."""
+    q, k, v, pages = np.ascontiguousarray(q), _c(k, np.float64), _c(v, np.float64), _c(pages, np.int32)
+    T, n_q, hd = q.shape
+    n_pages, n_kv, ps, _ = k.shape
+    out, mag = np.full((T, n_q, hd), np.nan), np.full((T, n_q, hd), np.nan)
+    lse, big = np.full((n_q, T), np.nan), np.full((n_q, T), np.nan)
+    cu, kv_len = _c(cu, np.int32), _c(kv_len, np.int32)
+    _load().oracle_attend(_p(q), T, n_q, hd, _p(cu), _p(kv_len), kv_len.size, _p(k), _p(v),
+                          _p(pages), n_pages, pages.shape[1], ps, n_kv, float(scale), int(window),
+                          _p(out), _p(lse), _p(mag), _p(big))
+    return out, lse, mag, big

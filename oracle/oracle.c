@@ -476,3 +476,105 @@ void oracle_compact(const uint8_t *const *seg, const int32_t *seg_bytes,
     }
     *head = h0 + i;
 }
+
+/* ------------------------------------------- attention of a serving step
+ *
+ * The rows at an attention hook (`.submodule("attention.post")`, Fig. 2) by
+ * their textbook definitions: root-mean-square norm of a head, rotary position
+ * embedding, softmax attention over the keys a token sees. */
+
+static double widen(const void *x, int is_bf16, int64_t i) {
+    return is_bf16 ? bf16_to_double(((const uint16_t *)x)[i]) : (double)((const float *)x)[i];
+}
+
+/* out[t,h,:] = rotate(x / sqrt(mean(x^2) + eps) * weight, pos[t]) unrounded, for
+ * tokens with pos >= 0; weight NULL: no norm; rot = 0: no rotation. */
+void oracle_norm_rope(const void *x, int is_bf16, int32_t T, int32_t n, int32_t hd,
+                      const int32_t *pos, const void *weight, double eps, const double *inv_freq,
+                      int32_t rot, int32_t pairs, double *out) {
+#pragma omp parallel for schedule(dynamic, 16)
+    for (int32_t t = 0; t < T; ++t) {
+        if (pos[t] < 0) continue;
+        for (int32_t h = 0; h < n; ++h) {
+            const int64_t base = ((int64_t)t * n + h) * hd;
+            double *y = out + base, r = 1.0;
+            if (weight) {
+                double s = 0.0;
+                for (int32_t i = 0; i < hd; ++i) {
+                    const double v = widen(x, is_bf16, base + i);
+                    s += v * v;
+                }
+                r = 1.0 / sqrt(s / hd + eps);
+            }
+            for (int32_t i = 0; i < hd; ++i)
+                y[i] = widen(x, is_bf16, base + i) * r * (weight ? widen(weight, is_bf16, i) : 1.0);
+            for (int32_t i = 0; i < rot / 2; ++i) {
+                const int32_t ia = pairs ? 2 * i : i, ib = pairs ? 2 * i + 1 : i + rot / 2;
+                const double c = cos(pos[t] * inv_freq[i]), s = sin(pos[t] * inv_freq[i]);
+                const double a = y[ia], b = y[ib];
+                y[ia] = a * c - b * s;
+                y[ib] = b * c + a * s;
+            }
+        }
+    }
+}
+
+/* Causal attention over a paged cache whose values are given widened (k, v
+ * [n_pages][n_kv][page_size][hd]).  Per token i of request r's span, at position
+ * p = kv_len[r] - n + i, over the keys j <= p (window > 0: j > p - window):
+ *   out = sum_j softmax(s)_j v_j,  lse = log sum_j exp(s_j),
+ *   mag = sum_j softmax(s)_j |v_j|, big = max_j scale * sum_c |q_c k_jc|
+ * (the last two bound what a rounding can do).  A page id out of range leaves its
+ * keys out.  out, mag [T][n_q][hd], lse, big [n_q][T]. */
+void oracle_attend(const uint16_t *q, int32_t T, int32_t n_q, int32_t hd, const int32_t *cu,
+                   const int32_t *kv_len, int32_t R, const double *k, const double *v,
+                   const int32_t *pages, int32_t n_pages, int32_t max_pages, int32_t page_size,
+                   int32_t n_kv, double scale, int32_t window, double *out, double *lse,
+                   double *mag, double *big) {
+    for (int32_t r = 0; r < R; ++r) {
+        const int32_t n = cu[r + 1] - cu[r];
+#pragma omp parallel for schedule(dynamic, 1)
+        for (int32_t e = 0; e < n * n_q; ++e) {
+            const int32_t i = e / n_q, g = e % n_q, head = g / (n_q / n_kv), t = cu[r] + i;
+            const int32_t p = kv_len[r] - n + i;
+            const int32_t first = window > 0 && p - window + 1 > 0 ? p - window + 1 : 0;
+            double *o = out + ((int64_t)t * n_q + g) * hd, *a = mag + ((int64_t)t * n_q + g) * hd;
+            double *s = malloc(sizeof(double) * (size_t)(p >= 0 ? p + 1 : 1));
+            double m = -INFINITY, top = 0.0, sum = 0.0;
+            for (int32_t j = first; j <= p; ++j) {
+                const int32_t page = pages[(int64_t)r * max_pages + j / page_size];
+                s[j] = -INFINITY;
+                if (page < 0 || page >= n_pages) continue;
+                const double *kr = k + (((int64_t)page * n_kv + head) * page_size + j % page_size) * hd;
+                double dot = 0.0, abs_ = 0.0;
+                for (int32_t c = 0; c < hd; ++c) {
+                    const double x = bf16_to_double(q[((int64_t)t * n_q + g) * hd + c]) * kr[c];
+                    dot += x;
+                    abs_ += fabs(x);
+                }
+                s[j] = scale * dot;
+                if (s[j] > m) m = s[j];
+                if (scale * abs_ > top) top = scale * abs_;
+            }
+            for (int32_t c = 0; c < hd; ++c) o[c] = a[c] = 0.0;
+            for (int32_t j = first; j <= p; ++j) {
+                if (s[j] == -INFINITY) continue;
+                const int32_t page = pages[(int64_t)r * max_pages + j / page_size];
+                const double *vr = v + (((int64_t)page * n_kv + head) * page_size + j % page_size) * hd;
+                const double w = exp(s[j] - m);
+                sum += w;
+                for (int32_t c = 0; c < hd; ++c) {
+                    o[c] += w * vr[c];
+                    a[c] += w * fabs(vr[c]);
+                }
+            }
+            for (int32_t c = 0; c < hd && sum > 0.0; ++c) {
+                o[c] /= sum;
+                a[c] /= sum;
+            }
+            lse[(int64_t)g * T + t] = sum > 0.0 ? m + log(sum) : -INFINITY;
+            big[(int64_t)g * T + t] = top;
+            free(s);
+        }
+    }
+}

@@ -34,9 +34,11 @@ _lib = ctypes.CDLL(LIB_PATH)
 from . import _call  # noqa: E402  (built beside the library)
 
 XMIX_OK, XMIX_E_INVAL, XMIX_E_UNSUPPORTED, XMIX_E_WORKSPACE, XMIX_E_LAUNCH = range(5)
-XMIX_F32, XMIX_BF16 = 0, 1
+XMIX_F32, XMIX_BF16, XMIX_E4M3 = 0, 1, 2
 XMIX_PROBE_TOKEN, XMIX_PROBE_MEAN, XMIX_PROBE_LAST = 0, 1, 2
 XMIX_ERR_REQUEST_RANGE, XMIX_ERR_T_VALID = 1, 2
+XMIX_ERR_KV_SLOT, XMIX_ERR_KV_SPAN, XMIX_ERR_KV_PAGE = 4, 8, 16
+XMIX_ROPE_HALF, XMIX_ROPE_PAIRS = 0, 1
 MAX_APPS, MAX_TOPK, MAX_CLAMP, MAX_SEGMENTS = 32, 64, 16, 4
 
 
@@ -75,7 +77,17 @@ class XmixSaeClampApp(ctypes.Structure):
                 ("delta_out", _vp)]
 
 
-_st = ctypes.c_int
+class XmixRope(ctypes.Structure):
+    _fields_ = [("inv_freq", _vp), ("rot_dim", _i32), ("pairing", _i32)]
+
+
+class XmixKvCache(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("pages", _vp), ("k_scale", _vp), ("v_scale", _vp),
+                ("n_pages", _i32), ("page_size", _i32), ("n_kv", _i32), ("head_dim", _i32),
+                ("R_max", _i32), ("max_pages", _i32), ("dt", ctypes.c_int)]
+
+
+_st, _i64, _f32 = ctypes.c_int, ctypes.c_int64, ctypes.c_float
 _sigs = {
     "xmix_status_string": ([_st], ctypes.c_char_p),
     "xmix_version": ([], ctypes.c_char_p),
@@ -129,6 +141,13 @@ _sigs = {
     "xmix_sae_fold_bias": ([_dp, _vp, _vp, _vp, _vp], _st),
     "xmix_sae_clamp_decode": ([_vp, _i32, ctypes.POINTER(XmixRoute), _i32, _vp, _vp, _i32, _vp,
                                _i32, _vp, _vp, _i32, _vp, _vp], _st),
+    "xmix_qk_norm_rope": ([_vp, _i64, _i32, _vp, _i64, _i32, _st, _i32, _i32, _vp, _vp, _vp, _f32,
+                           ctypes.POINTER(XmixRope), _vp, _i64, _vp, _i64, _vp, _vp], _st),
+    "xmix_kv_append": ([_vp, _i64, _vp, _i64, _st, _i32, _vp, _vp, ctypes.POINTER(XmixRope),
+                        ctypes.POINTER(XmixKvCache), _vp, _vp, _vp], _st),
+    "xmix_paged_attention_workspace": ([_i32, _i32, _i32, ctypes.POINTER(XmixKvCache)], _sz),
+    "xmix_paged_attention": ([_vp, _i64, _i32, _i32, _vp, _vp, ctypes.POINTER(XmixKvCache), _f32,
+                              _i32, _i32, _vp, _i64, _vp, _vp, _vp, _sz, _vp], _st),
     "xmix_readback_compact": ([_vp, _vp, _i32, ctypes.POINTER(XmixRoute), _i32, _vp, _i32, _i32,
                                ctypes.POINTER(XmixRing), _vp], _st),
 }
@@ -144,7 +163,8 @@ def _native(name: str, args: str, c_args: str):
     """The C entry point `name` behind native checks and marshalling: its Python
     arguments and the C arguments made of them, as csrc/call.cpp describes."""
     return _call.Function(name, ctypes.cast(getattr(_lib, name), _vp).value, args, c_args,
-                          {"Route": XmixRoute, "Ring": XmixRing, "Dict": XmixSaeDict})
+                          {"Route": XmixRoute, "Ring": XmixRing, "Dict": XmixSaeDict, "Rope": XmixRope,
+                           "Cache": XmixKvCache})
 
 
 _STEER = "vecs:A[...,d] sbits:bits(n) alpha:f32[R,n]"
@@ -195,6 +215,21 @@ _encode_topk_ring = _native(
     "xmix_sae_encode_topk_ring",
     f"{_ENCODE} req:i32{{T}} layer:int app:int ring:struct(Ring) stream:stream",
     f"{_ENCODE_C} req layer app ring stream")
+_qk_norm_rope = _native(
+    "xmix_qk_norm_rope",
+    "q:A~[T,n,D] k?:A~[T,m,D] pos:i32[T] q_w?:A[D] k_w?:A[D] eps:float rope?:struct(Rope) "
+    "q_out:A~[T,n,D] k_out?:A~[T,m,D] T_valid?:i32 stream:here",
+    "q /q n k /k m @A D T pos q_w k_w eps rope q_out /q_out k_out /k_out T_valid stream")
+_kv_append = _native(
+    "xmix_kv_append",
+    "k:A~[T,n,D] v:A~[T,n,D] req:i32[T] pos:i32[T] rope?:struct(Rope) cache:struct(Cache) n:dim "
+    "D:dim err?:i32 T_valid?:i32 stream:here",
+    "k /k v /v @A T req pos rope cache err T_valid stream")
+_paged_attention = _native(
+    "xmix_paged_attention",
+    "q:bf16~[T,n,D] cu:i32 kv_len:i32[R] cache:struct(Cache) R:dim D:dim scale:float window:int "
+    "max_q:int out:bf16~[T,n,D] lse?:f32[n,T] err?:i32 ws?:* stream:here",
+    "q /q n T cu kv_len cache scale window max_q out /out lse err ws %ws stream")
 _graph_launch = _native("xmix_graph_launch", "graph:int stream:stream", "graph stream")
 
 
@@ -265,6 +300,51 @@ class Ring:
         self.head = torch.zeros(2, dtype=torch.int64, device=device)
         self.struct = XmixRing(self.slots.data_ptr(), self.head.data_ptr(), self.capacity,
                                self.row_bytes)
+
+
+class Rope:
+    """A position rotation of the first ``2 * len(inv_freq)`` values of a head:
+    inv_freq fp64 [rot_dim / 2] on the device, radians per position."""
+
+    def __init__(self, inv_freq: torch.Tensor, pairing: int = XMIX_ROPE_HALF):
+        if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1:
+            raise TypeError("inv_freq must be a float64 vector")
+        self.inv_freq, self.rot_dim, self.pairing = inv_freq, 2 * inv_freq.numel(), int(pairing)
+        self.struct = XmixRope(_ptr(inv_freq), self.rot_dim, self.pairing)
+
+
+class KvCache:
+    """The paged cache of one layer: k and v [n_pages, n_kv, page_size, head_dim]
+    bf16 or float8_e4m3fn, pages int32 [R_max, max_pages] (the page ids of each
+    request, in order), and for 8-bit values the fp32 scales [n_kv] of the heads
+    (ones where none are given)."""
+
+    def __init__(self, k, v, pages, k_scale=None, v_scale=None):
+        if k.dtype not in (torch.bfloat16, torch.float8_e4m3fn) or v.dtype != k.dtype:
+            raise TypeError("cached keys and values are bfloat16 or float8_e4m3fn, both the same")
+        if k.dim() != 4 or v.shape != k.shape or pages.dim() != 2 or pages.dtype != torch.int32:
+            raise ValueError("k and v are [n_pages, n_kv, page_size, head_dim], pages int32 "
+                             "[R_max, max_pages]")
+        n_pages, n_kv, page_size, head_dim = k.shape
+        if k.dtype == torch.bfloat16:
+            if k_scale is not None or v_scale is not None:
+                raise ValueError("bfloat16 values have no scales")
+        else:
+            k_scale, v_scale = [torch.ones(n_kv, device=k.device) if s is None else s
+                                for s in (k_scale, v_scale)]
+            for s in (k_scale, v_scale):
+                if s.dtype != torch.float32 or s.shape != (n_kv,):
+                    raise ValueError("scales are float32 [n_kv]")
+        own = [x for x in (k, v, pages, k_scale, v_scale) if x is not None]
+        if any(x.device != k.device for x in own):
+            raise ValueError("the cache's tensors must live on one device")
+        self.k, self.v, self.pages, self.k_scale, self.v_scale = k, v, pages, k_scale, v_scale
+        self.n_kv, self.head_dim, self.R_max = n_kv, head_dim, pages.shape[0]
+        self.device = k.device
+        self.struct = XmixKvCache(_ptr(k), _ptr(v), _ptr(pages), _ptr(k_scale), _ptr(v_scale),
+                                  n_pages, page_size, n_kv, head_dim, pages.shape[0],
+                                  pages.shape[1],
+                                  XMIX_BF16 if k.dtype == torch.bfloat16 else XMIX_E4M3)
 
 
 # ------------------------------------------------------------------ entries
@@ -632,3 +712,39 @@ def xmix_readback_compact(segments: Sequence[torch.Tensor], route: Route, app_bi
     _check("xmix_readback_compact", _lib.xmix_readback_compact(
         ptrs, sizes, n, ctypes.byref(route.struct), app_bit, _ptr(req_of_token), layer_id,
         app_id, ctypes.byref(ring.struct), _stream(stream)))
+
+
+def xmix_qk_norm_rope(q, k, pos_of_token, q_weight, k_weight, eps: float, rope: Optional[Rope],
+                      q_out, k_out, T_valid=None, stream=None):
+    """Norm of every head (weight [head_dim]; None: none) and position rotation
+    (None: none) in one pass: q [T_max, n_q, head_dim], k [T_max, n_kv, head_dim]
+    bf16/fp32 (k and k_out None: queries alone) into q_out and k_out, which may be
+    q and k.  Rows may lie any distance apart; pos_of_token int32 [T_max], a
+    negative one leaves its row out."""
+    _check("xmix_qk_norm_rope", _qk_norm_rope(q, k, pos_of_token, q_weight, k_weight, eps, rope,
+                                              q_out, k_out, T_valid, stream))
+
+
+def xmix_kv_append(k, v, req_of_token, pos_of_token, rope: Optional[Rope], cache: KvCache, err_word,
+                   T_valid=None, stream=None):
+    """The keys (rotated by `rope`; None: as they are) and values of a step,
+    [T_max, n_kv, head_dim] bf16/fp32, into the pages of their requests."""
+    _check("xmix_kv_append", _kv_append(k, v, req_of_token, pos_of_token, rope, cache, cache.n_kv,
+                                        cache.head_dim, err_word, T_valid, stream))
+
+
+def paged_attention_workspace(T_max: int, n_q: int, max_q: int, cache: KvCache) -> int:
+    return int(_lib.xmix_paged_attention_workspace(T_max, n_q, max_q, ctypes.byref(cache.struct)))
+
+
+def xmix_paged_attention(q, cu_seqlens, kv_len, cache: KvCache, scale: float, window: int,
+                         max_q: int, out, lse_out, err_word, ws, stream=None):
+    """Attention of the tokens q [T_max, n_q, head_dim] bf16 over the pages of
+    their requests into out (the same shape; lse_out fp32 [n_q, T_max] or None).
+    cu_seqlens int32 [R_max + 1], kv_len int32 [R_max] (cached keys, the step's own
+    among them); window: the keys a token sees at most, itself among them (0: all);
+    max_q: no span is longer; ws: uint8, paged_attention_workspace bytes."""
+    assert cu_seqlens.numel() == cache.R_max + 1
+    _check("xmix_paged_attention", _paged_attention(
+        q, cu_seqlens, kv_len, cache, cache.R_max, cache.head_dim, scale, window, max_q, out,
+        lse_out, err_word, ws, stream))

@@ -571,3 +571,152 @@ xmix_status xmix_readback_compact(const void* const* seg_rows, const int32_t* se
 }
 
 }  // extern "C"
+
+// ------------------------------------------------ attention of a serving step
+
+namespace {
+
+// A rotation of at most head_dim values as the kernels take it; NULL: none.
+bool rope_ok(const xmix_rope* rope, int32_t head_dim, RopeIn* out) {
+    out->inv_freq = nullptr;
+    out->rot_dim = out->pairs = 0;
+    if (!rope) return true;
+    if (!rope->inv_freq || !aligned16(rope->inv_freq) || rope->rot_dim < 16 ||
+        rope->rot_dim % 16 != 0 || rope->rot_dim > head_dim ||
+        (rope->pairing != XMIX_ROPE_HALF && rope->pairing != XMIX_ROPE_PAIRS))
+        return false;
+    out->inv_freq = rope->inv_freq;
+    out->rot_dim = rope->rot_dim;
+    out->pairs = rope->pairing == XMIX_ROPE_PAIRS;
+    return true;
+}
+
+bool head_dim_ok(int32_t hd) { return hd >= 16 && hd <= 256 && hd % 16 == 0; }
+
+// Rows of n heads whose starts are 16-byte aligned.  A row of an output holds its
+// heads; an input's rows may overlap (an expanded tensor).
+bool rows_ok(const void* p, int64_t stride, int32_t n, int32_t hd, int32_t size, bool out) {
+    return p && aligned16(p) && n >= 1 && stride >= (out ? static_cast<int64_t>(n) * hd : 0) &&
+           stride * size % 16 == 0 && stride <= (int64_t{1} << 40);
+}
+
+bool cache_ok(const xmix_kv_cache* c, KvCacheIn* out) {
+    if (!c || !c->k || !c->v || !c->pages || !aligned16(c->k) || !aligned16(c->v)) return false;
+    if (c->dt != XMIX_BF16 && c->dt != XMIX_E4M3) return false;
+    if ((c->dt == XMIX_E4M3) != (c->k_scale != nullptr) ||
+        (c->dt == XMIX_E4M3) != (c->v_scale != nullptr))
+        return false;
+    if (c->n_pages < 1 || c->n_kv < 1 || c->R_max < 1 || c->max_pages < 1 || c->page_size < 16 ||
+        c->page_size > 4096 || (c->page_size & (c->page_size - 1)) != 0 ||
+        !head_dim_ok(c->head_dim))
+        return false;
+    if (static_cast<int64_t>(c->max_pages) * c->page_size > INT32_MAX) return false;
+    out->k = c->k;
+    out->v = c->v;
+    out->pages = c->pages;
+    out->k_scale = c->k_scale;
+    out->v_scale = c->v_scale;
+    out->n_pages = c->n_pages;
+    out->page_log2 = __builtin_ctz(static_cast<unsigned>(c->page_size));
+    out->n_kv = c->n_kv;
+    out->head_dim = c->head_dim;
+    out->R_max = c->R_max;
+    out->max_pages = c->max_pages;
+    return true;
+}
+
+bool attend_heads_ok(int32_t n_q, int32_t max_q, const KvCacheIn& c) {
+    return n_q >= 1 && n_q % c.n_kv == 0 && max_q >= 1;
+}
+bool attend_supported(const KvCacheIn& c) {
+    return (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256) && c.R_max <= 4096;
+}
+
+}  // namespace
+
+extern "C" {
+
+xmix_status xmix_qk_norm_rope(const void* q, int64_t q_stride, int32_t n_q, const void* k,
+                              int64_t k_stride, int32_t n_kv, xmix_dtype dt, int32_t head_dim,
+                              int32_t T_max, const int32_t* pos_of_token, const void* q_weight,
+                              const void* k_weight, float eps, const xmix_rope* rope, void* q_out,
+                              int64_t q_out_stride, void* k_out, int64_t k_out_stride,
+                              const int32_t* T_valid, void* stream) {
+    if (dt != XMIX_BF16 && dt != XMIX_F32) return XMIX_E_INVAL;
+    const int32_t size = dt == XMIX_BF16 ? 2 : 4;
+    RopeIn r;
+    if (!head_dim_ok(head_dim) || T_max < 1 || !pos_of_token || !(eps >= 0.0f) ||
+        !rope_ok(rope, head_dim, &r))
+        return XMIX_E_INVAL;
+    if (!rows_ok(q, q_stride, n_q, head_dim, size, false) ||
+        !rows_ok(q_out, q_out_stride, n_q, head_dim, size, true) || !aligned16(q_weight))
+        return XMIX_E_INVAL;
+    if (n_kv != 0 || k || k_out)
+        if (!rows_ok(k, k_stride, n_kv, head_dim, size, false) ||
+            !rows_ok(k_out, k_out_stride, n_kv, head_dim, size, true) || !aligned16(k_weight))
+            return XMIX_E_INVAL;
+    const HeadRows qr{q, q_weight, q_out, q_stride, q_out_stride, n_q};
+    const HeadRows kr{k, k_weight, k_out, k_stride, k_out_stride, n_kv};
+    return launched(launch_norm_rope(qr, kr, dt == XMIX_BF16, head_dim, T_max, pos_of_token, T_valid,
+                                     eps, r, as_stream(stream)));
+}
+
+xmix_status xmix_kv_append(const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                           xmix_dtype dt, int32_t T_max, const int32_t* req_of_token,
+                           const int32_t* pos_of_token, const xmix_rope* rope,
+                           const xmix_kv_cache* cache, uint32_t* err_word,
+                           const int32_t* T_valid, void* stream) {
+    if (dt != XMIX_BF16 && dt != XMIX_F32) return XMIX_E_INVAL;
+    const int32_t size = dt == XMIX_BF16 ? 2 : 4;
+    KvCacheIn c;
+    RopeIn r;
+    if (!cache_ok(cache, &c) || T_max < 1 || !req_of_token || !pos_of_token || !err_word ||
+        !rope_ok(rope, c.head_dim, &r) || !rows_ok(k, k_stride, c.n_kv, c.head_dim, size, false) ||
+        !rows_ok(v, v_stride, c.n_kv, c.head_dim, size, false))
+        return XMIX_E_INVAL;
+    return launched(launch_kv_append(k, k_stride, v, v_stride, dt == XMIX_BF16, T_max, req_of_token,
+                                     pos_of_token, T_valid, r, c, cache->dt == XMIX_E4M3, err_word,
+                                     as_stream(stream)));
+}
+
+size_t xmix_paged_attention_workspace(int32_t T_max, int32_t n_q, int32_t max_q,
+                                      const xmix_kv_cache* cache) {
+    KvCacheIn c;
+    if (T_max < 1 || !cache_ok(cache, &c) || !attend_heads_ok(n_q, max_q, c) ||
+        !attend_supported(c))
+        return 0;
+    return attend_workspace(n_q, max_q, c);
+}
+
+xmix_status xmix_paged_attention(const uint16_t* q, int64_t q_stride, int32_t n_q, int32_t T_max,
+                                 const int32_t* cu_seqlens, const int32_t* kv_len,
+                                 const xmix_kv_cache* cache, float scale, int32_t window,
+                                 int32_t max_q, uint16_t* out, int64_t out_stride, float* lse_out,
+                                 uint32_t* err_word, void* ws, size_t ws_bytes, void* stream) {
+    KvCacheIn c;
+    if (!cache_ok(cache, &c) || T_max < 1 || !cu_seqlens || !kv_len || !err_word || window < 0 ||
+        !(scale > 0.0f) || scale > 3.4e38f || !attend_heads_ok(n_q, max_q, c) ||
+        !rows_ok(q, q_stride, n_q, c.head_dim, 2, false) ||
+        !rows_ok(out, out_stride, n_q, c.head_dim, 2, true))
+        return XMIX_E_INVAL;
+    if (!attend_supported(c)) return XMIX_E_UNSUPPORTED;
+    const size_t need = attend_workspace(n_q, max_q, c);
+    if (need && (!ws || !aligned16(ws) || ws_bytes < need)) return XMIX_E_WORKSPACE;
+    AttendIn in;
+    in.q = q;
+    in.q_stride = q_stride;
+    in.cu = cu_seqlens;
+    in.kv_len = kv_len;
+    in.out = out;
+    in.out_stride = out_stride;
+    in.lse = lse_out;
+    in.err_word = err_word;
+    in.n_q = n_q;
+    in.T_max = T_max;
+    in.window = window;
+    in.max_q = max_q;
+    in.scale = scale;
+    return launched(launch_attend(in, c, cache->dt == XMIX_E4M3, ws, as_stream(stream)));
+}
+
+}  // extern "C"

@@ -14,17 +14,24 @@
 //                     dim^: a Route is passed on with at most so many slots, so
 //                     that a kernel which reads all rows of its slots stays inside
 //                     a tensor of fewer rows
+//   name:dtype~[dims] the rows (the first dim) may lie any distance apart, each
+//                     of them contiguous
 //   name?:...         the same, or None (a null pointer)
 //   name:struct(S)    an object whose `struct` is of the ctypes class given for S;
 //                     that struct is passed
 //   name:rt(S)        the same, its T_max bound to T
 //   name:bits(n)      a sequence of ints (at most 32 pass); n is bound to its length
+//   name?:struct(S)   the same, or None (a null pointer)
 //   name:int          an int
+//   name:float        a float
 //   name:dim          an int that the dim of this name is bound to
 //   name:stream       None (the current stream), a torch stream or a handle
 //                     (anything that int() takes)
+//   name:here         the same, and every tensor lives on the current device
 // C arguments: an argument's name, a bound dim, @L (the type code of letter L),
-// #name (the element count of a tensor), %name (its bytes, 0 for None).
+// #name (the element count of a tensor), %name (its bytes, 0 for None), /name
+// (the distance of its rows in elements).  Floats stand among them in the order
+// of the Python arguments.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <structmember.h>
@@ -41,9 +48,9 @@
 
 namespace {
 
-constexpr int kMaxArgs = 24, kMaxDims = 12, kMaxBits = 32, kMaxBitArgs = 2;
+constexpr int kMaxArgs = 24, kMaxDims = 12, kMaxBits = 32, kMaxBitArgs = 2, kMaxFloats = 2;
 
-enum Kind { TENSOR, STRUCT, BITS, INT, STREAM };
+enum Kind { TENSOR, STRUCT, BITS, INT, FLOAT, STREAM };
 enum { ANY_TYPE = -1, LETTER = -2 };
 
 struct Arg {
@@ -53,13 +60,15 @@ struct Arg {
     int dtype = ANY_TYPE;  // at::ScalarType, ANY_TYPE or LETTER
     int letter = 0;
     bool tail = false, count = false, shaped = false;
+    bool rows = false;          // TENSOR: a row distance of its own
+    bool here = false;          // STREAM: tensors of the current device only
     int cut = -1;               // the dim with a ^
     std::vector<int64_t> dims;  // >= 0: a number; -1: any; <= -2: name -2 - v
     int bind = -1;              // STRUCT, BITS, INT: the dim that is bound (-1: none)
     PyTypeObject* type = nullptr;  // STRUCT: the class of the struct (a reference)
 };
 struct Out {
-    enum What { ARG, DIM, TYPE, COUNT, BYTES } what;
+    enum What { ARG, DIM, TYPE, COUNT, BYTES, ROWS } what;
     int i;
 };
 
@@ -109,6 +118,17 @@ bool attr_u64(PyObject* o, PyObject* name, uint64_t* v) {
     return !PyErr_Occurred();
 }
 
+// The distance of the rows of t in elements, or -1 if a row is not contiguous.
+// (Where there is one row at most it is that row's length.)
+int64_t row_distance(const at::Tensor& t) {
+    int64_t want = 1;
+    for (int64_t k = t.dim() - 1; k > 0; --k) {
+        if (t.size(k) != 1 && t.stride(k) != want) return -1;
+        want *= t.size(k);
+    }
+    return t.dim() > 0 && t.size(0) > 1 ? t.stride(0) : want;
+}
+
 PyObject* call(PyObject* self, PyObject* const* argv, size_t nargsf, PyObject* kwnames) {
     HANDLE_TH_ERRORS  // a tensor without storage throws when asked for its data
     Function* f = reinterpret_cast<Function*>(self);
@@ -118,7 +138,9 @@ PyObject* call(PyObject* self, PyObject* const* argv, size_t nargsf, PyObject* k
         return PyErr_Format(PyExc_TypeError, "%s takes %zu positional arguments", f->name->c_str(),
                             args.size());
     uint64_t value[kMaxArgs];
-    int64_t count[kMaxArgs], bytes[kMaxArgs], dims[kMaxDims];
+    int64_t count[kMaxArgs], bytes[kMaxArgs], rows[kMaxArgs], dims[kMaxDims];
+    float floats[kMaxFloats] = {};
+    int n_floats = 0, device = -1;
     int letters[26];
     int32_t bits[kMaxBitArgs][kMaxBits];
     int n_bits = 0;
@@ -131,7 +153,7 @@ PyObject* call(PyObject* self, PyObject* const* argv, size_t nargsf, PyObject* k
         const Arg& a = args[i];
         PyObject* o = argv[i];
         value[i] = 0;
-        count[i] = bytes[i] = 0;
+        count[i] = bytes[i] = rows[i] = 0;
         switch (a.kind) {
             case TENSOR: {
                 if (o == Py_None && a.optional) break;
@@ -141,10 +163,18 @@ PyObject* call(PyObject* self, PyObject* const* argv, size_t nargsf, PyObject* k
                     PyErr_SetString(PyExc_ValueError, "tensor must live on the GPU");
                     return nullptr;
                 }
-                if (!t.is_contiguous()) {
+                if (a.rows) {
+                    rows[i] = row_distance(t);
+                    if (rows[i] < 0) {
+                        PyErr_SetString(PyExc_ValueError, "rows of the tensor must be contiguous");
+                        return nullptr;
+                    }
+                } else if (!t.is_contiguous()) {
                     PyErr_SetString(PyExc_ValueError, "tensor must be contiguous");
                     return nullptr;
                 }
+                const int at_device = t.get_device();
+                device = device < 0 || device == at_device ? at_device : INT32_MAX;
                 const int type = static_cast<int>(t.scalar_type());
                 if (a.dtype == LETTER) {
                     int& l = letters[a.letter];
@@ -177,6 +207,7 @@ PyObject* call(PyObject* self, PyObject* const* argv, size_t nargsf, PyObject* k
                 break;
             }
             case STRUCT: {
+                if (o == Py_None && a.optional) break;
                 PyObject* st = PyObject_GetAttr(o, s_struct);
                 if (!st) return nullptr;
                 held.o[held.n++] = st;
@@ -221,8 +252,23 @@ PyObject* call(PyObject* self, PyObject* const* argv, size_t nargsf, PyObject* k
                 if (a.bind >= 0 && !bind(dims, a.bind, v)) return fail(f, a, "wrong size");
                 break;
             }
+            case FLOAT: {
+                floats[n_floats++] = static_cast<float>(PyFloat_AsDouble(o));
+                if (PyErr_Occurred()) return nullptr;
+                break;
+            }
             case STREAM: {
                 PyObject* s = nullptr;
+                if (a.here && device >= 0) {
+                    PyObject* dev = PyObject_CallNoArgs(get_device);
+                    if (!dev) return nullptr;
+                    const long current = PyLong_AsLong(dev);
+                    Py_DECREF(dev);
+                    if (current != device) {
+                        PyErr_SetString(PyExc_ValueError, "tensors must live on the current device");
+                        return nullptr;
+                    }
+                }
                 if (o == Py_None) {
                     PyObject* dev = PyObject_CallNoArgs(get_device);
                     if (!dev) return nullptr;
@@ -264,18 +310,21 @@ PyObject* call(PyObject* self, PyObject* const* argv, size_t nargsf, PyObject* k
                 break;
             case Out::COUNT: c[i] = static_cast<uint64_t>(count[o.i]); break;
             case Out::BYTES: c[i] = static_cast<uint64_t>(bytes[o.i]); break;
+            case Out::ROWS: c[i] = static_cast<uint64_t>(rows[o.i]); break;
         }
     }
     // Every C argument is a pointer or an integer of at most 64 bits, so each
     // takes one register or one eight-byte stack slot (System V x86-64), and
-    // slots past the callee's own are not looked at.
+    // slots past the callee's own are not looked at.  Its floats are in the vector
+    // registers, in their own order wherever they stand among the others.
     using U = uint64_t;
-    using Fn = int (*)(U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U);
+    using Fn = int (*)(U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, float,
+                       float);
     int st;
     Py_BEGIN_ALLOW_THREADS
     st = reinterpret_cast<Fn>(f->addr)(
         c[0], c[1], c[2], c[3], c[4], c[5], c[6], c[7], c[8], c[9], c[10], c[11], c[12], c[13],
-        c[14], c[15], c[16], c[17], c[18], c[19], c[20], c[21], c[22], c[23]);
+        c[14], c[15], c[16], c[17], c[18], c[19], c[20], c[21], c[22], c[23], floats[0], floats[1]);
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(st);
     END_HANDLE_TH_ERRORS
@@ -325,14 +374,21 @@ struct Parser {
         } else if (t == "int" || t == "dim") {
             a->kind = INT;
             if (t == "dim") a->bind = dim(a->name);
-        } else if (t == "stream") {
+        } else if (t == "float") {
+            a->kind = FLOAT;
+        } else if (t == "stream" || t == "here") {
             a->kind = STREAM;
+            a->here = t == "here";
         } else if (t.rfind("bits(", 0) == 0 && t.back() == ')') {
             a->kind = BITS;
             a->bind = dim(t.substr(5, t.size() - 6));
         } else {
             const size_t open = t.find_first_of("[{");
-            const std::string type = t.substr(0, open);
+            std::string type = t.substr(0, open);
+            if (!type.empty() && type.back() == '~') {
+                a->rows = true;
+                type.pop_back();
+            }
             if (type == "i32") a->dtype = static_cast<int>(at::kInt);
             else if (type == "f32") a->dtype = static_cast<int>(at::kFloat);
             else if (type == "bf16") a->dtype = static_cast<int>(at::kBFloat16);
@@ -379,7 +435,7 @@ int init(PyObject* self, PyObject* args, PyObject*) {
     f->args = new std::vector<Arg>;
     f->outs = new std::vector<Out>;
     Parser p{structs};
-    int bit_args = 0;
+    int bit_args = 0, float_args = 0;
     bool cut = false;
     for (const std::string& w : words(in, ' ')) {
         Arg a;
@@ -388,6 +444,7 @@ int init(PyObject* self, PyObject* args, PyObject*) {
             return -1;
         }
         bit_args += a.kind == BITS;
+        float_args += a.kind == FLOAT;
         Py_XINCREF(a.type);
         cut = cut || a.cut >= 0;
         f->args->push_back(a);
@@ -402,11 +459,14 @@ int init(PyObject* self, PyObject* args, PyObject*) {
         if (w[0] == '@') o = {Out::TYPE, w[1] - 'A'};
         else if (w[0] == '#') o = {Out::COUNT, arg_of(w.substr(1))};
         else if (w[0] == '%') o = {Out::BYTES, arg_of(w.substr(1))};
+        else if (w[0] == '/') o = {Out::ROWS, arg_of(w.substr(1))};
         else if (o.i < 0 && p.dim_of.count(w)) o = {Out::DIM, p.dim_of[w]};
         if (o.i < 0) {
             PyErr_Format(PyExc_ValueError, "%s: unknown C argument '%s'", name, w.c_str());
             return -1;
         }
+        // floats go to registers of their own, in the order of the Python arguments
+        if (o.what == Out::ARG && (*f->args)[o.i].kind == FLOAT) continue;
         f->outs->push_back(o);
     }
     f->n_dims = static_cast<int>(p.dim_of.size());
@@ -416,7 +476,7 @@ int init(PyObject* self, PyObject* args, PyObject*) {
         return -1;
     }
     if (f->args->size() > kMaxArgs || f->outs->size() > kMaxArgs || f->n_dims > kMaxDims ||
-        bit_args > kMaxBitArgs) {
+        bit_args > kMaxBitArgs || float_args > kMaxFloats) {
         PyErr_Format(PyExc_ValueError, "%s: too many arguments", name);
         return -1;
     }

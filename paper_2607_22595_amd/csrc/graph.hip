@@ -51,6 +51,8 @@ const std::vector<KernelInfo>& kernel_table() {
         add_sae_kernels(t);
         add_clamp_kernels(t);
         add_compact_kernels(t);
+        add_head_kernels(t);
+        add_attend_kernels(t);
         return t;
     }();
     return table;

@@ -1,0 +1,189 @@
+// Per-head passes of an attention layer's rows: norm and position rotation of
+// queries and keys, and the append of keys and values to the paged cache.
+//
+// Both read every value once and write it once, so memory bounds them (and at
+// decode sizes the latency of one chain: position, rows, result).
+#include "common.hpp"
+#include "kernels.hpp"
+#include "launch.hpp"
+#include "paged.hpp"
+#include "rope.hpp"
+
+namespace xmix {
+
+template <>
+struct ArgPointers<RopeIn> {
+    static std::vector<uint16_t> offsets() { return {offsetof(RopeIn, inv_freq)}; }
+};
+template <>
+struct ArgPointers<HeadRows> {
+    static std::vector<uint16_t> offsets() {
+        return {offsetof(HeadRows, x), offsetof(HeadRows, weight), offsetof(HeadRows, out)};
+    }
+};
+constexpr int kHeadThreads = 256;
+
+// Sum over the n lanes (a power of two up to 16) that share a head.
+__device__ __forceinline__ float head_sum(float v, int n) {
+    if (n > 1) v += dpp_f<kDppXor1>(v);
+    if (n > 2) v += dpp_f<kDppXor2>(v);
+    if (n > 4) v += dpp_f<kDppHalfMirror>(v);
+    if (n > 8) v += dpp_f<kDppMirror>(v);
+    return v;
+}
+
+// One workgroup per token.  Its lanes form groups of one head each, which take
+// the token's query heads and then its key heads in turn; a lane's angles are
+// computed once for all of them.
+//   y = x (mean(x^2) + eps)^(-1/2) w,   out = round(rotate(y))
+template <bool BF16>
+__global__ void __launch_bounds__(kHeadThreads)
+norm_rope_kernel(HeadRows q, HeadRows k, int32_t head_dim, int32_t lanes_log2,
+                 const int32_t* __restrict__ pos_of_token, const int32_t* __restrict__ T_valid,
+                 float eps, RopeIn rope) {
+    const int32_t t = blockIdx.x, pos = pos_of_token[t];
+    if (pos < 0 || (T_valid && t >= *T_valid)) return;
+    const int lanes = 1 << lanes_log2, u = threadIdx.x & (lanes - 1);
+    const bool mine = 2 * kChunk * u < head_dim;
+    const HeadPart part = head_part(u, rope);
+    Angles g;
+    if (part.turned) angles(g, rope, u, pos);
+    constexpr int kBytes = BF16 ? 2 : 4;
+    for (int h = threadIdx.x >> lanes_log2; h < q.n + k.n; h += kHeadThreads >> lanes_log2) {
+        const bool is_q = h < q.n;
+        const HeadRows& r = is_q ? q : k;
+        const int64_t in_row = (is_q ? h : h - q.n) * static_cast<int64_t>(head_dim);
+        const char* x = static_cast<const char*>(r.x) + (t * r.stride + in_row) * kBytes;
+        float a[kChunk] = {}, b[kChunk] = {};
+        if (mine) {
+            const Raw<BF16> ra = load_chunk<BF16>(x, part.a), rb = load_chunk<BF16>(x, part.b);
+            widen<BF16>(ra, a);
+            widen<BF16>(rb, b);
+        }
+        if (r.weight) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) sum += a[i] * a[i] + b[i] * b[i];
+            sum = head_sum(sum, lanes);
+            const float inv = 1.0f / sqrtf(sum / static_cast<float>(head_dim) + eps);
+            if (mine) {
+                float wa[kChunk], wb[kChunk];
+                widen<BF16>(load_chunk<BF16>(r.weight, part.a), wa);
+                widen<BF16>(load_chunk<BF16>(r.weight, part.b), wb);
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) {
+                    a[i] = a[i] * inv * wa[i];
+                    b[i] = b[i] * inv * wb[i];
+                }
+            }
+        }
+        if (!mine) continue;
+        if (part.turned) rotate(a, b, g, rope.pairs != 0);
+        char* out = static_cast<char*>(r.out) + (t * r.out_stride + in_row) * kBytes;
+        store_chunk<BF16>(out, part.a, a);
+        store_chunk<BF16>(out, part.b, b);
+    }
+}
+
+hipError_t launch_norm_rope(const HeadRows& q, const HeadRows& k, bool bf16, int32_t head_dim,
+                            int32_t T_max, const int32_t* pos, const int32_t* T_valid, float eps,
+                            const RopeIn& rope, hipStream_t stream) {
+    int lg = 0;
+    while ((1 << lg) < head_lanes(head_dim)) ++lg;
+    if (bf16)
+        hipLaunchKernelGGL(norm_rope_kernel<true>, dim3(T_max), dim3(kHeadThreads), 0, stream, q, k,
+                           head_dim, lg, pos, T_valid, eps, rope);
+    else
+        hipLaunchKernelGGL(norm_rope_kernel<false>, dim3(T_max), dim3(kHeadThreads), 0, stream, q, k,
+                           head_dim, lg, pos, T_valid, eps, rope);
+    return hipGetLastError();
+}
+
+// x / scale held to what the 8-bit type can represent (the conversion itself
+// turns larger values into NaN); NaN stays NaN.
+__device__ __forceinline__ float to_e4m3_range(float x, float scale) {
+    const float y = x / scale;
+    const float held = fminf(fmaxf(y, -448.0f), 448.0f);
+    return y == y ? held : y;
+}
+__device__ __forceinline__ uint32_t pack4_e4m3(const float* x) {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+    return __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], lo, true);
+}
+
+// One workgroup per token: its lane groups take the token's key heads, rotated,
+// and its value heads in turn, and store each into the token's slot.
+template <bool BF16, bool E4M3>
+__global__ void __launch_bounds__(kHeadThreads)
+kv_append_kernel(const void* __restrict__ k, int64_t k_stride, const void* __restrict__ v,
+                 int64_t v_stride, int32_t lanes_log2, const int32_t* __restrict__ req_of_token,
+                 const int32_t* __restrict__ pos_of_token, const int32_t* __restrict__ T_valid,
+                 RopeIn rope, KvCacheIn cache, uint32_t* __restrict__ err_word) {
+    const int32_t t = blockIdx.x, req = req_of_token[t], pos = pos_of_token[t];
+    if (req < 0 || pos < 0 || (T_valid && t >= *T_valid)) return;
+    int32_t page = -1;
+    const int32_t nth = pos >> cache.page_log2;
+    if (req < cache.R_max && nth < cache.max_pages)
+        page = page_at(cache, req, nth);
+    if (!page_ok(cache, page)) {
+        if (threadIdx.x == 0) atomicOr(err_word, kErrKvSlot);
+        return;
+    }
+    const int32_t hd = cache.head_dim, slot = pos & ((1 << cache.page_log2) - 1);
+    const int lanes = 1 << lanes_log2, u = threadIdx.x & (lanes - 1);
+    if (2 * kChunk * u >= hd) return;
+    const HeadPart part = head_part(u, rope);
+    Angles g;
+    if (part.turned) angles(g, rope, u, pos);
+    for (int h = threadIdx.x >> lanes_log2; h < 2 * cache.n_kv; h += kHeadThreads >> lanes_log2) {
+        const bool is_k = h < cache.n_kv;
+        const int head = is_k ? h : h - cache.n_kv;
+        const char* x = static_cast<const char*>(is_k ? k : v) +
+                        (t * (is_k ? k_stride : v_stride) + static_cast<int64_t>(head) * hd) *
+                            (BF16 ? 2 : 4);
+        float a[kChunk], b[kChunk];
+        const Raw<BF16> ra = load_chunk<BF16>(x, part.a), rb = load_chunk<BF16>(x, part.b);
+        widen<BF16>(ra, a);
+        widen<BF16>(rb, b);
+        if (is_k && part.turned) rotate(a, b, g, rope.pairs != 0);
+        const int64_t row = page_row(cache, page, head, slot);
+        char* out = static_cast<char*>(is_k ? cache.k : cache.v) + row * hd * (E4M3 ? 1 : 2);
+        if constexpr (E4M3) {
+            const float scale = (is_k ? cache.k_scale : cache.v_scale)[head];
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) {
+                a[i] = to_e4m3_range(a[i], scale);
+                b[i] = to_e4m3_range(b[i], scale);
+            }
+            *reinterpret_cast<uint2*>(out + part.a) = make_uint2(pack4_e4m3(a), pack4_e4m3(a + 4));
+            *reinterpret_cast<uint2*>(out + part.b) = make_uint2(pack4_e4m3(b), pack4_e4m3(b + 4));
+        } else {
+            store_chunk<true>(out, part.a, a);
+            store_chunk<true>(out, part.b, b);
+        }
+    }
+}
+
+hipError_t launch_kv_append(const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                            bool bf16, int32_t T_max, const int32_t* req, const int32_t* pos,
+                            const int32_t* T_valid, const RopeIn& rope, const KvCacheIn& cache,
+                            bool e4m3, uint32_t* err_word, hipStream_t stream) {
+    int lg = 0;
+    while ((1 << lg) < head_lanes(cache.head_dim)) ++lg;
+    const auto kernel = bf16 ? (e4m3 ? kv_append_kernel<true, true> : kv_append_kernel<true, false>)
+                             : (e4m3 ? kv_append_kernel<false, true> : kv_append_kernel<false, false>);
+    hipLaunchKernelGGL(kernel, dim3(T_max), dim3(kHeadThreads), 0, stream, k, k_stride, v, v_stride,
+                       lg, req, pos, T_valid, rope, cache, err_word);
+    return hipGetLastError();
+}
+
+void add_head_kernels(std::vector<KernelInfo>& t) {
+    t.push_back(kernel_info(norm_rope_kernel<true>));
+    t.push_back(kernel_info(norm_rope_kernel<false>));
+    t.push_back(kernel_info(kv_append_kernel<true, true>));
+    t.push_back(kernel_info(kv_append_kernel<true, false>));
+    t.push_back(kernel_info(kv_append_kernel<false, true>));
+    t.push_back(kernel_info(kv_append_kernel<false, false>));
+}
+
+}  // namespace xmix

@@ -46,5 +46,7 @@ void add_router_kernels(std::vector<KernelInfo>& t);
 void add_sae_kernels(std::vector<KernelInfo>& t);
 void add_clamp_kernels(std::vector<KernelInfo>& t);
 void add_compact_kernels(std::vector<KernelInfo>& t);
+void add_head_kernels(std::vector<KernelInfo>& t);
+void add_attend_kernels(std::vector<KernelInfo>& t);
 
 }  // namespace xmix

@@ -165,4 +165,56 @@ hipError_t launch_compact(const Segments& segs, const int32_t* app_count,
                           int32_t layer_id, int32_t app_id, uint8_t* slots, uint64_t* head,
                           int32_t capacity, int32_t row_bytes, hipStream_t stream);
 
+// ------------------------------------------------ attention of a serving step
+// Device error bits of the header, for kernels.
+constexpr uint32_t kErrKvSlot = 4u, kErrKvSpan = 8u, kErrKvPage = 16u;
+
+// One side of the norm and rotation pass: n heads a token, or none.
+struct HeadRows {
+    const void* x;
+    const void* weight;  // NULL: no norm
+    void* out;
+    int64_t stride, out_stride;  // elements from a token's row to the next one's
+    int32_t n;
+};
+// A position rotation (rot_dim 0: none).
+struct RopeIn {
+    const double* inv_freq;
+    int32_t rot_dim;
+    int32_t pairs;
+};
+// A paged cache as the kernels take it.
+struct KvCacheIn {
+    void* k;
+    void* v;
+    const int32_t* pages;
+    const float* k_scale;
+    const float* v_scale;
+    int32_t n_pages, page_log2, n_kv, head_dim, R_max, max_pages;
+};
+hipError_t launch_norm_rope(const HeadRows& q, const HeadRows& k, bool bf16, int32_t head_dim,
+                            int32_t T_max, const int32_t* pos, const int32_t* T_valid, float eps,
+                            const RopeIn& rope, hipStream_t stream);
+hipError_t launch_kv_append(const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                            bool bf16, int32_t T_max, const int32_t* req, const int32_t* pos,
+                            const int32_t* T_valid, const RopeIn& rope, const KvCacheIn& cache,
+                            bool e4m3, uint32_t* err_word, hipStream_t stream);
+
+// One attention call: rows of queries over the pages of their requests.
+struct AttendIn {
+    const uint16_t* q;
+    int64_t q_stride;
+    const int32_t* cu;
+    const int32_t* kv_len;
+    uint16_t* out;
+    int64_t out_stride;
+    float* lse;  // may be NULL
+    uint32_t* err_word;
+    int32_t n_q, T_max, window, max_q;
+    float scale;
+};
+size_t attend_workspace(int32_t n_q, int32_t max_q, const KvCacheIn& cache);
+hipError_t launch_attend(const AttendIn& in, const KvCacheIn& cache, bool e4m3, void* ws,
+                         hipStream_t stream);
+
 }  // namespace xmix
