@@ -3,8 +3,27 @@
 //   s_j = scale (q . k_j),  out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m)
 //
 // over the keys j that the token sees, in one pass with the running maximum m and
-// the running sum.  One wave per token and query head: a lane takes a key of each
-// 64, then each lane its columns of the values.
+// the running sum of each row.  A row is a (token, query head) pair; the rows of one
+// key head belong together, since they read the same keys.
+//
+// Both products are matrix instructions with the keys along the first axis of the
+// first and the rows along its second, S^T = K Q^T, then O^T = V^T P^T: a lane holds
+// the scores of one row, so maximum, exponential and rescaling are per lane, and
+// the weights it computes are already the operand of the second product (its sum
+// over the keys takes them in any order, as long as V^T comes in the same one).
+// V^T is read from LDS by the transposing reads (ds_read_tr).
+//
+// Work is dealt in blocks of 64 keys.  A unit is one key head of one request and a
+// tile of its rows; the blocks of all units, one behind the other, are cut into equal
+// ranges, one per workgroup, whatever the lengths are.  A unit that is cut leaves a
+// part (maximum, sum, O) per workgroup in the workspace, and the last workgroup to
+// finish one joins them in order.  attend_plan_kernel finds where each range starts.
+//
+// Two forms of the inner loop:
+//   tile kernel   128 rows a unit; the workgroup's four waves take 32 rows each and
+//                 share K and V in LDS (chunks of a prompt, mixed batches)
+//   row kernel    16 or 32 rows a unit; the waves take keys of their own (decode and
+//                 drafted tokens, where the cache is read once and memory is the bound)
 #include "common.hpp"
 #include "kernels.hpp"
 #include "launch.hpp"
@@ -20,82 +39,1007 @@ struct ArgPointers<AttendIn> {
     }
 };
 
-template <bool E4M3>
-__device__ __forceinline__ float cached(const void* p, int64_t at) {
-    if constexpr (E4M3)
-        return __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t*>(p)[at], 0);
-    else
-        return bf16_to_f32(static_cast<const uint16_t*>(p)[at]);
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
+
+constexpr int kAttendThreads = 256, kAttendWaves = 4;
+constexpr int kBlockKeys = 64;     // keys of a block
+constexpr int kGroupKeys = 16;     // keys that surely lie in one page
+constexpr int kTileRows = 128;     // rows of a unit of the tile kernel
+constexpr int kMaxRequests = 4096;
+constexpr int kPlanThreads = 1024;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+// A running maximum is raised only by a score this far above it (powers of two): the
+// weights stay below 2^8, which neither fp32 sums nor bf16 weights mind, and the
+// rescaling of O, rare after the first blocks, is skipped by a wave vote.
+constexpr float kRaise = 8.0f;
+
+struct WorkStart {  // where a workgroup's range begins
+    int32_t req, head, tile, block;
+};
+struct PlanHead {
+    int64_t blocks, share;  // of all units; of one workgroup
+};
+// The workspace: plan head, a start per workgroup, a count of finished parts per
+// workgroup that begins a cut unit, and two parts per workgroup.
+struct AttendWs {
+    PlanHead* head;
+    WorkStart* start;
+    int32_t* done;
+    float* parts;
+};
+template <>
+struct ArgPointers<AttendWs> {
+    static std::vector<uint16_t> offsets() {
+        return {offsetof(AttendWs, head), offsetof(AttendWs, start), offsetof(AttendWs, done),
+                offsetof(AttendWs, parts)};
+    }
+};
+
+// ------------------------------------------------------------------- geometry
+
+// A request's span and keys; n = 0 where it has no rows to write.
+struct Span {
+    int32_t lo, n, len;
+};
+__device__ __forceinline__ Span span_of(const AttendIn& in, const KvCacheIn& c, int32_t r,
+                                        bool* bad = nullptr) {
+    const int32_t lo = in.cu[r], hi = in.cu[r + 1], len = in.kv_len[r];
+    Span s{lo, 0, len};
+    if (lo < 0 || hi < lo || hi > in.T_max) {
+        if (bad) *bad = true;
+        return s;
+    }
+    if (hi == lo) return s;
+    if (hi - lo > in.max_q || len < 0 || len > c.max_pages << c.page_log2) {
+        if (bad) *bad = true;
+        return s;
+    }
+    s.n = hi - lo;
+    return s;
+}
+__device__ __forceinline__ int32_t tiles_of(int32_t n, int32_t group, int32_t rows) {
+    return static_cast<int32_t>((static_cast<int64_t>(n) * group + rows - 1) / rows);
+}
+// The keys that some row of tile t sees, in blocks: [first, first + count), one block
+// at least (a tile without a key still has rows to write).
+struct Blocks {
+    int32_t first, count;
+};
+__device__ __forceinline__ Blocks blocks_of(const Span& s, int32_t t, int32_t group, int32_t rows,
+                                            int32_t window) {
+    const int32_t tok0 = t * rows / group, tok1 = min(((t + 1) * rows - 1) / group, s.n - 1);
+    const int32_t hi = s.len - s.n + tok1 + 1, p0 = s.len - s.n + tok0;
+    const int32_t lo = window > 0 && p0 >= window ? p0 - window + 1 : 0;
+    const int32_t first = hi > 0 ? lo / kBlockKeys : 0;
+    const int32_t end = hi > 0 ? (hi + kBlockKeys - 1) / kBlockKeys : 1;
+    return {first, end - first};
 }
 
-template <bool E4M3>
-__global__ void __launch_bounds__(kWave)
-attend_kernel(AttendIn in, KvCacheIn cache) {
-    const int32_t r = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
-    const int32_t lo = in.cu[r], hi = in.cu[r + 1], n = hi - lo, len = in.kv_len[r];
-    if (n == 0 && lo >= 0 && lo <= in.T_max) return;
-    if (lo < 0 || hi > in.T_max || n < 0 || n > in.max_q || len < 0 ||
-        (len >> cache.page_log2) + ((len & ((1 << cache.page_log2) - 1)) != 0) > cache.max_pages) {
-        if (lane == 0) atomicOr(in.err_word, kErrKvSpan);
-        return;
+// ----------------------------------------------------------------------- plan
+
+__device__ __forceinline__ int64_t wave_sum64(int64_t v) {
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// One workgroup.  Blocks of each request (a thread each, or where a request has
+// many tiles a wave each), their prefix, then the start of every range by a search
+// in the prefix and a walk over the request's tiles.
+__global__ void __launch_bounds__(kPlanThreads)
+attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int32_t n_wg,
+                   int32_t least, int32_t many) {
+    __shared__ int64_t upto[kMaxRequests + 1];
+    __shared__ int64_t wave_total[kPlanThreads / kWave];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int32_t R = cache.R_max, group = in.n_q / cache.n_kv;
+    bool bad = false;
+    if (!many) {
+        for (int32_t r = tid; r < R; r += kPlanThreads) {
+            const Span s = span_of(in, cache, r, &bad);
+            const int32_t tiles = tiles_of(s.n, group, rows);
+            int64_t sum = 0;
+            for (int32_t t = 0; t < tiles; ++t) sum += blocks_of(s, t, group, rows, in.window).count;
+            upto[r + 1] = sum * cache.n_kv;
+        }
+    } else {
+        for (int32_t r = wave; r < R; r += kPlanThreads / kWave) {
+            const Span s = span_of(in, cache, r, &bad);
+            const int32_t tiles = tiles_of(s.n, group, rows);
+            int64_t sum = 0;
+            for (int32_t t = lane; t < tiles; t += kWave)
+                sum += blocks_of(s, t, group, rows, in.window).count;
+            sum = wave_sum64(sum);
+            if (lane == 0) upto[r + 1] = sum * cache.n_kv;
+        }
     }
-    const int32_t hd = cache.head_dim, head = h / (in.n_q / cache.n_kv);
-    const float ks = E4M3 ? cache.k_scale[head] : 1.0f, vs = E4M3 ? cache.v_scale[head] : 1.0f;
-    constexpr int kCols = 4;  // of 64 lanes: head_dim up to 256
-    for (int32_t i = blockIdx.z; i < n; i += gridDim.z) {
-        const int32_t p = len - n + i;
-        const uint16_t* q = in.q + (lo + i) * in.q_stride + static_cast<int64_t>(h) * hd;
-        float m = -INFINITY, l = 0.0f, acc[kCols] = {};
-        const int32_t first = in.window > 0 && p >= in.window ? p - in.window + 1 : 0;
-        for (int32_t j0 = first; j0 <= p; j0 += kWave) {
-            const int32_t j = min(j0 + lane, p);
-            const int32_t page = page_at(cache, r, j >> cache.page_log2);
-            const bool ok = page_ok(cache, page);
-            if (!ok) atomicOr(in.err_word, kErrKvPage);
-            const int64_t row = page_row(cache, ok ? page : 0, head, j & ((1 << cache.page_log2) - 1)) * hd;
-            float s = 0.0f;
-            for (int c = 0; c < hd; ++c) s += bf16_to_f32(q[c]) * cached<E4M3>(cache.k, row + c);
-            s *= in.scale * ks;
-            if (j0 + lane > p || !ok) s = -INFINITY;
-            float top = s;
-            for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-            const float m2 = fmaxf(m, top), base = m2 == -INFINITY ? 0.0f : m2;
-            const float e = expf(s - base), fade = expf(m - base);
-            m = m2;
-            l = l * fade + wave_sum(e);
-            for (int c = 0; c < kCols; ++c) acc[c] *= fade;
-            for (int k = 0; k < kWave; ++k) {
-                const float w = __shfl(e, k);
-                const int64_t at = __shfl(row, k);
-                if (j0 + k > p || !__shfl(ok, k)) continue;
-                for (int c = 0; c < kCols; ++c)
-                    if (lane + c * kWave < hd) acc[c] += w * cached<E4M3>(cache.v, at + lane + c * kWave);
+    if (bad) atomicOr(in.err_word, kErrKvSpan);
+    if (tid == 0) upto[0] = 0;
+    __syncthreads();
+    // prefix over the requests, four to a thread
+    constexpr int kEach = kMaxRequests / kPlanThreads;
+    int64_t v[kEach], sum = 0;
+    for (int i = 0; i < kEach; ++i) {
+        const int32_t r = tid * kEach + i;
+        sum += r < R ? upto[r + 1] : 0;
+        v[i] = sum;
+    }
+    int64_t incl = sum;
+    for (int o = 1; o < kWave; o <<= 1) {
+        const int64_t up = __shfl_up(incl, o);
+        if (lane >= o) incl += up;
+    }
+    if (lane == kWave - 1) wave_total[wave] = incl;
+    __syncthreads();
+    int64_t before = incl - sum;
+    for (int w = 0; w < wave; ++w) before += wave_total[w];
+    for (int i = 0; i < kEach; ++i)
+        if (tid * kEach + i < R) upto[tid * kEach + i + 1] = before + v[i];
+    __syncthreads();
+    const int64_t blocks = upto[R];
+    const int64_t share = max(static_cast<int64_t>(least), (blocks + n_wg - 1) / n_wg);
+    if (tid == 0) *ws.head = PlanHead{blocks, share};
+    for (int32_t w = tid; w < n_wg; w += kPlanThreads) {
+        ws.done[w] = 0;
+        const int64_t at = w * share;
+        if (at >= blocks) continue;
+        int32_t lo = 0, hi = R - 1;  // the last request that starts at or before `at`
+        while (lo < hi) {
+            const int32_t mid = (lo + hi + 1) >> 1;
+            if (upto[mid] <= at) lo = mid;
+            else hi = mid - 1;
+        }
+        const Span s = span_of(in, cache, lo);
+        const int64_t a_head = (upto[lo + 1] - upto[lo]) / cache.n_kv, rest = at - upto[lo];
+        WorkStart st{lo, static_cast<int32_t>(rest / a_head), 0, 0};
+        int64_t left = rest % a_head;
+        for (;;) {
+            const int32_t count = blocks_of(s, st.tile, group, rows, in.window).count;
+            if (left < count) break;
+            left -= count;
+            ++st.tile;
+        }
+        st.block = static_cast<int32_t>(left);
+        ws.start[w] = st;
+    }
+}
+
+// ------------------------------------------------------------- cached values
+
+// Rows of one head of the cache in LDS: how the 16-byte pieces of a row are permuted
+// (the copies into LDS place each piece linearly, so it is the source address that
+// is permuted), such that the lanes of one read cover all banks.
+//   K (both kernels): 16 lanes read one piece each of 16 rows
+//   V: the transposing reads take 4 rows of 32 bytes (bf16) or 8 of 16 bytes (e4m3)
+//   per 16 lanes; which rows and columns 32 lanes take differs between the kernels
+template <int RB>
+__device__ __forceinline__ int swz_k(int row) {
+    constexpr int per = RB >= 256 ? 1 : 256 / RB, mask = RB >= 256 ? 15 : RB / 16 - 1;
+    return (row / per) & mask;
+}
+template <int RB, bool E4M3>
+__device__ __forceinline__ int swz_v_tile(int row) {
+    if constexpr (!E4M3) return RB >= 256 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
+    else if constexpr (RB >= 256) return (row & 3) << 1 | ((row >> 3) & 1) << 3;
+    else if constexpr (RB == 128) return ((row >> 1) & 1) << 1 | ((row >> 3) & 1) << 2;
+    else return ((row >> 3) & 1) << 1;
+}
+template <int RB, bool E4M3>
+__device__ __forceinline__ int swz_v_row(int row) {
+    if constexpr (!E4M3) return RB >= 256 ? (row & 7) << 1 : ((row >> 1) & 3) << 1;
+    else if constexpr (RB >= 256) return (row & 7) | ((row >> 4) & 1) << 3;
+    else if constexpr (RB == 128) return ((row >> 1) & 3) | ((row >> 4) & 1) << 2;
+    else return ((row >> 2) & 1) | ((row >> 4) & 1) << 1;
+}
+
+// A buffer resource over the rows of one head that hold the keys from `key` on, of
+// at most 16 (one page): past the request's last key, and in a page that is not
+// there, it reads zeros and touches no memory.
+template <int RB>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t group_rows(const void* base, const KvCacheIn& c,
+                                                             int32_t page, int32_t head,
+                                                             int32_t key, int32_t len) {
+    const bool ok = page_ok(c, page);
+    const int64_t row = page_row(c, ok ? page : 0, head, key & ((1 << c.page_log2) - 1));
+    const int32_t live = ok ? max(0, min(kGroupKeys, len - key)) : 0;
+    return __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char*>(static_cast<const char*>(base)) + row * RB, 0, live * RB, kBufferDword3);
+}
+// The page id of a key; past the request's last key, that one's.
+__device__ __forceinline__ int32_t page_of_key(const KvCacheIn& c, int32_t req, int32_t key,
+                                               int32_t len) {
+    const int32_t nth = max(0, min(key, len - 1)) >> c.page_log2;
+    return __builtin_amdgcn_readfirstlane(page_at(c, req, nth));
+}
+
+typedef __attribute__((address_space(3))) void* lds_ptr;
+typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4;
+typedef __attribute__((address_space(3))) i32x2_t* lds_i32x2;
+
+// Sixteen bytes per lane from `off` bytes into the resource to dst (uniform) + lane.
+__device__ __forceinline__ void copy16(__amdgpu_buffer_rsrc_t r, uint4* dst, int32_t off) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)dst, 16, off, 0, 0, 0);
+}
+__device__ __forceinline__ bf16x8_t as_bf16x8(const uint4& v) {
+    return __builtin_bit_cast(bf16x8_t, v);
+}
+// Eight e4m3 values, exactly.
+__device__ __forceinline__ bf16x8_t e4m3_to_bf16(int lo, int hi) {
+    uint4 w;
+    w.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false));
+    w.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true));
+    w.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false));
+    w.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
+    return as_bf16x8(w);
+}
+// Weights to bf16, nearest even: 2^-9 of each on average, which the sum over many
+// keys averages out; the sum of the weights keeps them in fp32.
+__device__ __forceinline__ uint32_t weights2(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{a, b}, bf16x2_t));
+}
+
+// Both halves' (lanes l and l ^ 32), and all four quarters', largest and sum.
+__device__ __forceinline__ float half_max(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float quarter_max(float v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return half_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float quarter_sum(float v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return half_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// A V^T operand taken apart: its finite values, and ones where a value is +inf
+// or NaN, and -inf or NaN.  A product with a masked key's weight (zero) must leave
+// nothing, which it does not where the value is not finite; rows that see the key
+// get their infinity by the counts.
+struct Apart {
+    bf16x8_t finite, up, down;
+};
+__device__ __forceinline__ Apart take_apart(const bf16x8_t& v) {
+    const uint4 w4 = __builtin_bit_cast(uint4, v);
+    const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+    uint32_t f[4], u[4], d[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[i] = u[i] = d[i] = 0;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t x = (w[i] >> (16 * e)) & 0xFFFFu;
+            const bool odd = (x & 0x7F80u) == 0x7F80u, nan = odd && (x & 0x7Fu);
+            f[i] |= (odd ? 0u : x) << (16 * e);
+            u[i] |= (odd && (nan || !(x & 0x8000u)) ? 0x3F80u : 0u) << (16 * e);
+            d[i] |= (odd && (nan || (x & 0x8000u)) ? 0x3F80u : 0u) << (16 * e);
+        }
+    }
+    return {as_bf16x8(make_uint4(f[0], f[1], f[2], f[3])), as_bf16x8(make_uint4(u[0], u[1], u[2], u[3])),
+            as_bf16x8(make_uint4(d[0], d[1], d[2], d[3]))};
+}
+__device__ __forceinline__ float with_counts(float o, float up, float down) {
+    return o + (up > 0.0f ? INFINITY : 0.0f) + (down > 0.0f ? -INFINITY : 0.0f);
+}
+
+// ------------------------------------------------------------- joining parts
+
+// A part: the rows' maxima (powers of two, -inf: no key) and sums, then O [row][HD].
+template <int M, int HD>
+struct Part {
+    static constexpr int kFloats = M * (HD + 2);
+    static __device__ float* at(const AttendWs& ws, int32_t wg, bool opens) {
+        return ws.parts + (2 * static_cast<int64_t>(wg) + (opens ? 1 : 0)) * kFloats;
+    }
+};
+
+// The rows of a unit in the caller's tensors.
+struct RowsOut {
+    int32_t lo, n_rows, row0, head, group;  // first token of the span; its rows; the tile's first
+};
+__device__ __forceinline__ uint16_t* out_row(const AttendIn& in, const RowsOut& u, int32_t row,
+                                             int hd) {
+    const int32_t at = u.row0 + row, tok = at / u.group, g = at - tok * u.group;
+    return in.out + (u.lo + tok) * in.out_stride + static_cast<int64_t>(u.head * u.group + g) * hd;
+}
+__device__ __forceinline__ void store_lse(const AttendIn& in, const RowsOut& u, int32_t row, float m,
+                                          float l) {
+    if (!in.lse) return;
+    const int32_t at = u.row0 + row, tok = at / u.group, g = at - tok * u.group;
+    in.lse[static_cast<int64_t>(u.head * u.group + g) * in.T_max + u.lo + tok] =
+        l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+__device__ __forceinline__ float weight_of(float m, float top) {
+    return m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+}
+
+// After this workgroup's part is written: the last of the unit's workgroups joins
+// the parts, in their order, and writes the rows.
+template <int M, int HD>
+__device__ void join_parts(const AttendIn& in, const AttendWs& ws, const RowsOut& u, int32_t first,
+                           int32_t last, float v_scale, int* flag) {
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) *flag = atomicAdd(ws.done + first, 1) == last - first;
+    __syncthreads();
+    if (!*flag) return;
+    __threadfence();
+    constexpr int kVec = HD / 4;
+    const int32_t rows = min(M, u.n_rows - u.row0);
+    for (int32_t e = threadIdx.x; e < rows * kVec; e += kAttendThreads) {
+        const int32_t row = e / kVec, c = e % kVec;
+        float top = -INFINITY, l = 0.0f;
+        f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int32_t w = first; w <= last; ++w) {
+            const float* p = Part<M, HD>::at(ws, w, w == first);
+            const float m = p[row], top2 = fmaxf(top, m);
+            const float a = weight_of(top, top2), b = weight_of(m, top2);
+            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(p + 2 * M + row * HD + 4 * c);
+            l = l * a + p[M + row] * b;
+            o = o * a + x * b;
+            top = top2;
+        }
+        const float inv = l == 0.0f ? 0.0f : v_scale / l;
+        *reinterpret_cast<uint2*>(out_row(in, u, row, HD) + 4 * c) =
+            make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+        if (c == 0) store_lse(in, u, row, top, l);
+    }
+}
+
+// The workgroups are dealt over the XCDs in turn; neighbouring ranges, which read the
+// same keys, go to one XCD and its L2.
+__device__ __forceinline__ int32_t range_of_block(int32_t n_wg) {
+    const int32_t b = blockIdx.x;
+    return n_wg % 8 == 0 ? (b % 8) * (n_wg / 8) + b / 8 : b;
+}
+
+// ---------------------------------------------------------------- tile kernel
+
+template <int HD, bool E4M3>
+__global__ void __launch_bounds__(kAttendThreads, HD > 128 ? 1 : 2)
+attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
+    constexpr int RB = HD * (E4M3 ? 1 : 2);      // bytes of a cached row
+    constexpr int kTile = kBlockKeys * RB / 16;  // pieces of a block
+    constexpr int kCopies = kGroupKeys * RB / 1024;
+    constexpr int kSteps = HD / 16, kCols = HD / 32;
+    __shared__ uint4 kA[kTile], kB[kTile], vA[kTile], vB[kTile];
+    __shared__ int flag;
+    const int32_t wg = range_of_block(n_wg);
+    const int64_t share = ws.head->share, blocks = ws.head->blocks;
+    int64_t at = wg * share;
+    const int64_t end = min(at + share, blocks);
+    if (at >= end) return;
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, n32 = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int32_t group = in.n_q / cache.n_kv;
+    WorkStart st = ws.start[wg];
+
+    // this lane's sources within a group of 16 rows, and its reads of a block
+    int32_t src_k[kCopies], src_v[kCopies];
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+        const int at16 = i * 64 + lane, row = at16 / (RB / 16), slot = at16 % (RB / 16);
+        src_k[i] = row * RB + ((slot ^ swz_k<RB>(row)) * 16);
+        src_v[i] = row * RB + ((slot ^ swz_v_tile<RB, E4M3>(row)) * 16);
+    }
+
+    while (at < end) {
+        const Span s = span_of(in, cache, st.req);
+        const int32_t tiles = tiles_of(s.n, group, kTileRows);
+        const Blocks bl = blocks_of(s, st.tile, group, kTileRows, in.window);
+        const int32_t count = static_cast<int32_t>(min(static_cast<int64_t>(bl.count - st.block), end - at));
+        const RowsOut u{s.lo, s.n * group, st.tile * kTileRows, st.head, group};
+        const float ks = E4M3 ? cache.k_scale[st.head] : 1.0f;
+        const float c2 = in.scale * ks * kLog2e;
+        // this lane's row, and the tokens of the wave's rows
+        const int32_t row = u.row0 + wave * 32 + n32;
+        const bool row_ok = row < u.n_rows;
+        const int32_t tok = min(row, u.n_rows - 1) / group;
+        const int32_t base = s.len - s.n;
+        const int32_t pos = base + tok;  // (rows past the last repeat it and are not stored)
+        const int32_t wrow0 = u.row0 + wave * 32;
+        const bool wave_on = wrow0 < u.n_rows;
+        const int32_t p_first = base + min(wrow0, u.n_rows - 1) / group;
+        const int32_t p_last = base + min(wrow0 + 31, u.n_rows - 1) / group;
+        bf16x8_t Q[kSteps];
+        {
+            const uint16_t* qr = in.q + (u.lo + tok) * in.q_stride +
+                                 static_cast<int64_t>(u.head * group + min(row, u.n_rows - 1) % group) * HD;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int c = E4M3 ? 4 * (i >> 1) + 2 * half + (i & 1) : 2 * i + half;
+                Q[i] = as_bf16x8(reinterpret_cast<const uint4*>(qr)[c]);
             }
         }
-        uint16_t* out = in.out + (lo + i) * in.out_stride + static_cast<int64_t>(h) * hd;
-        for (int c = 0; c < kCols; ++c)
-            if (lane + c * kWave < hd)
-                out[lane + c * kWave] = l == 0.0f ? 0 : f32_to_bf16_rne(acc[c] / l * vs);
-        if (in.lse && lane == 0)
-            in.lse[static_cast<int64_t>(h) * in.T_max + lo + i] = l == 0.0f ? -INFINITY : m + logf(l);
+
+        auto stage = [&](int32_t block, uint4* kd, uint4* vd) __attribute__((always_inline)) {
+            const int32_t key = block * kBlockKeys + wave * kGroupKeys;
+            const int32_t page = page_of_key(cache, st.req, key, s.len);
+            const __amdgpu_buffer_rsrc_t kr = group_rows<RB>(cache.k, cache, page, st.head, key, s.len);
+            const __amdgpu_buffer_rsrc_t vr = group_rows<RB>(cache.v, cache, page, st.head, key, s.len);
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i)
+                copy16(kr, kd + wave * (kTile / 4) + i * 64, src_k[i]);
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i)
+                copy16(vr, vd + wave * (kTile / 4) + i * 64, src_v[i]);
+        };
+
+        float m, l;
+        f32x16_t O[kCols];
+        // One block: scores, weights, O.  CAREFUL: values that are not finite may stand
+        // in masked places.
+        auto block_step = [&](auto careful, int32_t block, const uint4* kt, const uint4* vt)
+            __attribute__((always_inline)) {
+            constexpr bool CAREFUL = decltype(careful)::value;
+            const int32_t key0 = block * kBlockKeys;
+            if (!wave_on || key0 > p_last) return;
+            f32x16_t S[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                f32x16_t acc = {};
+                const int kr = 32 * b + n32;
+                const uint4* krow = kt + kr * (RB / 16);
+                if constexpr (E4M3) {
+#pragma unroll
+                    for (int i = 0; i < kSteps / 2; ++i) {
+                        const uint4 w = krow[(2 * i + half) ^ swz_k<RB>(kr)];
+                        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e4m3_to_bf16(w.x, w.y), Q[2 * i], acc, 0, 0, 0);
+                        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e4m3_to_bf16(w.z, w.w), Q[2 * i + 1], acc, 0, 0, 0);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kSteps; ++i)
+                        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            as_bf16x8(krow[(2 * i + half) ^ swz_k<RB>(kr)]), Q[i], acc, 0, 0, 0);
+                }
+                S[b] = acc;
+            }
+            // pages that are not there, by groups of 16 keys
+            uint32_t gone = 0;
+#pragma unroll
+            for (int g = 0; g < kBlockKeys / kGroupKeys; ++g)
+                if (!page_ok(cache, page_of_key(cache, st.req, key0 + g * kGroupKeys, s.len)))
+                    gone |= 1u << g;
+            if (gone || key0 + kBlockKeys - 1 > p_first ||
+                (in.window > 0 && key0 <= p_last - in.window)) {
+                if (gone && lane == 0 && key0 < s.len) atomicOr(in.err_word, kErrKvPage);
+                const int32_t from = in.window > 0 ? pos - in.window : -1;
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int k = 32 * b + 8 * (i / 4) + 4 * half + i % 4;
+                        const bool see = key0 + k <= pos && key0 + k > from && !((gone >> (k / kGroupKeys)) & 1u);
+                        if (!see) S[b][i] = -INFINITY;
+                    }
+            }
+            float top = S[0][0];
+#pragma unroll
+            for (int i = 1; i < 32; ++i) top = fmaxf(top, S[i / 16][i % 16]);
+            top = half_max(top) * c2;
+            const bool raise = top > m + kRaise;
+            if (__any(raise)) {
+                const float m2 = raise ? top : m;
+                const float fade = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - m2);
+                m = m2;
+                l *= fade;
+#pragma unroll
+                for (int h = 0; h < kCols; ++h)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) O[h][i] *= fade;
+            }
+            const float off = m == -INFINITY ? 0.0f : m;
+            uint32_t P[2][8];
+            uint32_t seen[CAREFUL ? 2 : 1][8];
+            float sum = 0.0f;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(S[b][i], c2, -off));
+                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(S[b][i + 1], c2, -off));
+                    sum += x;
+                    sum += y;
+                    P[b][i / 2] = weights2(x, y);
+                    if constexpr (CAREFUL)
+                        seen[b][i / 2] = (S[b][i] == -INFINITY ? 0u : 0x3F80u) |
+                                         (S[b][i + 1] == -INFINITY ? 0u : 0x3F800000u);
+                }
+            l += sum;
+#pragma unroll
+            for (int h = 0; h < kCols; ++h) {
+                f32x16_t up = {}, down = {};
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int b = t / 2, i0 = 4 * (t % 2);
+                    const bf16x8_t w = as_bf16x8(make_uint4(P[b][i0], P[b][i0 + 1], P[b][i0 + 2], P[b][i0 + 3]));
+                    bf16x8_t v;
+                    const int i16 = lane & 15, side = (lane >> 4) & 1;
+                    if constexpr (E4M3) {
+                        const int r8 = i16 >> 1, kr = 16 * t + 8 * (r8 / 4) + 4 * half + r8 % 4;
+                        const uint4* p = vt + kr * (RB / 16) + ((2 * h + side) ^ swz_v_tile<RB, true>(kr));
+                        const i32x2_t x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                            (lds_i32x2)(reinterpret_cast<const char*>(p) + 8 * (i16 & 1)));
+                        v = e4m3_to_bf16(x[0], x[1]);
+                    } else {
+                        s16x4_t x[2];
+#pragma unroll
+                        for (int a = 0; a < 2; ++a) {
+                            const int kr = 16 * t + 8 * a + 4 * half + i16 / 4;
+                            const uint4* p = vt + kr * (RB / 16) +
+                                             ((4 * h + 2 * side + ((i16 & 3) >> 1)) ^ swz_v_tile<RB, false>(kr));
+                            x[a] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                (lds_s16x4)(reinterpret_cast<const char*>(p) + 8 * (i16 & 1)));
+                        }
+                        v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+                    }
+                    if constexpr (CAREFUL) {
+                        const Apart a = take_apart(v);
+                        const bf16x8_t one = as_bf16x8(make_uint4(seen[b][i0], seen[b][i0 + 1], seen[b][i0 + 2], seen[b][i0 + 3]));
+                        O[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.finite, w, O[h], 0, 0, 0);
+                        up = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.up, one, up, 0, 0, 0);
+                        down = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.down, one, down, 0, 0, 0);
+                    } else {
+                        O[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, O[h], 0, 0, 0);
+                    }
+                }
+                if constexpr (CAREFUL) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) O[h][i] = with_counts(O[h][i], up[i], down[i]);
+                }
+            }
+        };
+        auto run = [&](auto careful) __attribute__((always_inline)) {
+            m = -INFINITY;
+            l = 0.0f;
+#pragma unroll
+            for (int h = 0; h < kCols; ++h) O[h] = f32x16_t{};
+            const int32_t b0 = bl.first + st.block;
+            __syncthreads();  // the buffers are free
+            stage(b0, kA, vA);
+            for (int32_t i = 0; i < count; i += 2) {
+                __builtin_amdgcn_s_waitcnt(0);
+                __syncthreads();
+                if (i + 1 < count) stage(b0 + i + 1, kB, vB);
+                block_step(careful, b0 + i, kA, vA);
+                if (i + 1 >= count) break;
+                __builtin_amdgcn_s_waitcnt(0);
+                __syncthreads();
+                if (i + 2 < count) stage(b0 + i + 2, kA, vA);
+                block_step(careful, b0 + i + 1, kB, vB);
+            }
+        };
+        run(std::false_type{});
+        bool odd = false;
+#pragma unroll
+        for (int h = 0; h < kCols; ++h)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) odd |= !(fabsf(O[h][i]) < INFINITY);
+        if (__syncthreads_or(odd)) run(std::true_type{});
+        l = half_sum(l);
+
+        if (count == bl.count) {
+            if (row_ok) {
+                const float inv = l == 0.0f ? 0.0f : (E4M3 ? cache.v_scale[st.head] : 1.0f) / l;
+                uint16_t* out = out_row(in, u, wave * 32 + n32, HD);
+#pragma unroll
+                for (int h = 0; h < kCols; ++h)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        *reinterpret_cast<uint2*>(out + 32 * h + 2 * i + 4 * half) =
+                            make_uint2(pack_bf16(O[h][i] * inv, O[h][i + 1] * inv),
+                                       pack_bf16(O[h][i + 2] * inv, O[h][i + 3] * inv));
+                if (half == 0) store_lse(in, u, wave * 32 + n32, m, l);
+            }
+        } else {
+            float* part = Part<kTileRows, HD>::at(ws, wg, st.block == 0);
+            const int r = wave * 32 + n32;
+            if (half == 0) {
+                part[r] = m;
+                part[kTileRows + r] = l;
+            }
+#pragma unroll
+            for (int h = 0; h < kCols; ++h)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    *reinterpret_cast<f32x4_t*>(part + 2 * kTileRows + r * HD + 32 * h + 2 * i + 4 * half) =
+                        f32x4_t{O[h][i], O[h][i + 1], O[h][i + 2], O[h][i + 3]};
+            const int64_t begin = at - st.block;
+            join_parts<kTileRows, HD>(in, ws, u, static_cast<int32_t>(begin / share),
+                                      static_cast<int32_t>((begin + bl.count - 1) / share),
+                                      E4M3 ? cache.v_scale[st.head] : 1.0f, &flag);
+        }
+
+        at += count;
+        st.block = 0;
+        if (++st.tile == tiles) {
+            st.tile = 0;
+            if (++st.head == cache.n_kv) {
+                st.head = 0;
+                if (at < end)
+                    do ++st.req;
+                    while (span_of(in, cache, st.req).n == 0);
+            }
+        }
     }
 }
 
-size_t attend_workspace(int32_t, int32_t, const KvCacheIn&) { return 0; }
+// ----------------------------------------------------------------- row kernel
 
-hipError_t launch_attend(const AttendIn& in, const KvCacheIn& cache, bool e4m3, void*,
+template <int HD, bool E4M3, int NB>
+__global__ void __launch_bounds__(kAttendThreads, HD > 128 ? 1 : 2)
+attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
+    constexpr int RB = HD * (E4M3 ? 1 : 2);
+    constexpr int KS = !E4M3 && RB >= 256 ? 32 : 64;  // keys of a step: 8 KB of V, or more
+    constexpr int kGroups = KS / kGroupKeys;
+    constexpr int kLoads = RB / 64;               // 16-byte loads of a lane per 16 keys
+    constexpr int kCopies = kGroupKeys * RB / 1024;
+    constexpr int kSteps = HD / 32, kCols = HD / 16, M = 16 * NB;
+    constexpr int kTile = KS * RB / 16;           // pieces of a step's V
+    static_assert(kAttendWaves * kTile >= kAttendWaves * 16 * HD / 4, "room to join the waves");
+    __shared__ uint4 vA[kAttendWaves * kTile], vB[kAttendWaves * kTile];
+    __shared__ float wm[kAttendWaves][M], wl[kAttendWaves][M];
+    __shared__ int flag;
+    const int32_t wg = range_of_block(n_wg);
+    const int64_t share = ws.head->share, blocks = ws.head->blocks;
+    int64_t at = wg * share;
+    const int64_t end = min(at + share, blocks);
+    if (at >= end) return;
+    const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, n16 = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int32_t group = in.n_q / cache.n_kv;
+    WorkStart st = ws.start[wg];
+
+    // sources of V's copies, by their place in the step; swz_v_row takes the row's
+    // bits up to 4, so groups of 16 rows come in two kinds
+    int32_t src_v[2][kCopies];
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            const int at16 = i * 64 + lane, row = at16 / (RB / 16), slot = at16 % (RB / 16);
+            src_v[g][i] = row * RB + ((slot ^ swz_v_row<RB, E4M3>(16 * g + row)) * 16);
+        }
+    uint4* const vmA = vA + wave * kTile;
+    uint4* const vmB = vB + wave * kTile;
+
+    while (at < end) {
+        const Span s = span_of(in, cache, st.req);
+        const Blocks bl = blocks_of(s, 0, group, M, in.window);
+        const int32_t count = static_cast<int32_t>(min(static_cast<int64_t>(bl.count - st.block), end - at));
+        const RowsOut u{s.lo, s.n * group, 0, st.head, group};
+        const float c2 = in.scale * (E4M3 ? cache.k_scale[st.head] : 1.0f) * kLog2e;
+        const int32_t base = s.len - s.n;
+        const int32_t p_first = base, p_last = s.len - 1;
+        int32_t pos[NB];
+        bf16x8_t Q[NB][kSteps];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int32_t row = 16 * b + n16, held = min(row, u.n_rows - 1), tok = held / group;
+            pos[b] = base + tok;  // (rows past the last repeat it and are not stored)
+            const uint16_t* qr = in.q + (u.lo + tok) * in.q_stride +
+                                 static_cast<int64_t>(u.head * group + held % group) * HD;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int c = E4M3 ? 8 * (i >> 1) + 2 * g4 + (i & 1) : 4 * i + g4;
+                Q[b][i] = as_bf16x8(reinterpret_cast<const uint4*>(qr)[c]);
+            }
+        }
+        // this wave's steps: of the segment's, every fourth
+        const int32_t key_from = (bl.first + st.block) * kBlockKeys;
+        const int32_t steps = count * (kBlockKeys / KS);
+
+        uint4 KA[kGroups][kLoads], KB[kGroups][kLoads];
+        uint32_t goneA, goneB;
+        auto stage = [&](int32_t step, uint4 (&K)[kGroups][kLoads], uint4* vd, uint32_t& gone)
+            __attribute__((always_inline)) {
+            const int32_t key0 = key_from + step * KS;
+            gone = 0;
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const int32_t key = key0 + g * kGroupKeys;
+                const int32_t page = page_of_key(cache, st.req, key, s.len);
+                if (!page_ok(cache, page)) gone |= 1u << g;
+                const __amdgpu_buffer_rsrc_t kr = group_rows<RB>(cache.k, cache, page, st.head, key, s.len);
+                const __amdgpu_buffer_rsrc_t vr = group_rows<RB>(cache.v, cache, page, st.head, key, s.len);
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    const u32x4_t w = __builtin_bit_cast(
+                        u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(kr, n16 * RB + (4 * i + g4) * 16, 0, 0));
+                    K[g][i] = make_uint4(w.x, w.y, w.z, w.w);
+                }
+#pragma unroll
+                for (int i = 0; i < kCopies; ++i)
+                    copy16(vr, vd + g * (kGroupKeys * RB / 16) + i * 64, src_v[g & 1][i]);
+            }
+        };
+
+        float m[NB], l[NB];
+        f32x4_t O[NB][kCols];
+        auto key_step = [&](auto careful, int32_t step, const uint4 (&K)[kGroups][kLoads], const uint4* vt,
+                            uint32_t gone) __attribute__((always_inline)) {
+            constexpr bool CAREFUL = decltype(careful)::value;
+            const int32_t key0 = key_from + step * KS;
+            f32x4_t S[NB][kGroups];
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) S[b][g] = f32x4_t{};
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    bf16x8_t k;
+                    if constexpr (E4M3) {
+                        const uint4 w = K[g][i >> 1];
+                        k = i & 1 ? e4m3_to_bf16(w.z, w.w) : e4m3_to_bf16(w.x, w.y);
+                    } else {
+                        k = as_bf16x8(K[g][i]);
+                    }
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+                        S[b][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, Q[b][i], S[b][g], 0, 0, 0);
+                }
+            }
+            if (gone || key0 + KS - 1 > p_first || (in.window > 0 && key0 <= p_last - in.window)) {
+                if (gone && lane == 0 && key0 < s.len) atomicOr(in.err_word, kErrKvPage);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const int32_t from = in.window > 0 ? pos[b] - in.window : -1;
+#pragma unroll
+                    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int32_t k = key0 + 16 * g + 4 * g4 + i;
+                            if (!(k <= pos[b] && k > from && !((gone >> g) & 1u))) S[b][g][i] = -INFINITY;
+                        }
+                }
+            }
+            uint32_t P[NB][kGroups][2], seen[CAREFUL ? NB : 1][kGroups][2];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                float top = S[b][0][0];
+#pragma unroll
+                for (int i = 1; i < 4 * kGroups; ++i) top = fmaxf(top, S[b][i / 4][i % 4]);
+                top = quarter_max(top) * c2;
+                const bool raise = top > m[b] + kRaise;
+                if (__any(raise)) {
+                    const float m2 = raise ? top : m[b];
+                    const float fade = m[b] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[b] - m2);
+                    m[b] = m2;
+                    l[b] *= fade;
+#pragma unroll
+                    for (int h = 0; h < kCols; ++h) O[b][h] *= fade;
+                }
+                const float off = m[b] == -INFINITY ? 0.0f : m[b];
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(S[b][g][2 * i], c2, -off));
+                        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(S[b][g][2 * i + 1], c2, -off));
+                        l[b] += x + y;
+                        P[b][g][i] = weights2(x, y);
+                        if constexpr (CAREFUL)
+                            seen[b][g][i] = (S[b][g][2 * i] == -INFINITY ? 0u : 0x3F80u) |
+                                            (S[b][g][2 * i + 1] == -INFINITY ? 0u : 0x3F800000u);
+                    }
+            }
+#pragma unroll
+            for (int h = 0; h < kCols; ++h) {
+                f32x4_t up[NB], down[NB];
+#pragma unroll
+                for (int b = 0; b < NB; ++b) up[b] = down[b] = f32x4_t{};
+#pragma unroll
+                for (int t = 0; t < kGroups / 2; ++t) {
+                    bf16x8_t v;
+                    if constexpr (E4M3) {
+                        const int r8 = n16 >> 1, kr = 32 * t + 16 * (r8 / 4) + 4 * g4 + r8 % 4;
+                        const uint4* p = vt + kr * (RB / 16) + (h ^ swz_v_row<RB, true>(kr));
+                        const i32x2_t x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                            (lds_i32x2)(reinterpret_cast<const char*>(p) + 8 * (n16 & 1)));
+                        v = e4m3_to_bf16(x[0], x[1]);
+                    } else {
+                        s16x4_t x[2];
+#pragma unroll
+                        for (int a = 0; a < 2; ++a) {
+                            const int kr = 32 * t + 16 * a + 4 * g4 + n16 / 4;
+                            const uint4* p = vt + kr * (RB / 16) +
+                                             ((2 * h + ((n16 & 3) >> 1)) ^ swz_v_row<RB, false>(kr));
+                            x[a] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                (lds_s16x4)(reinterpret_cast<const char*>(p) + 8 * (n16 & 1)));
+                        }
+                        v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+                    }
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        const bf16x8_t w = as_bf16x8(make_uint4(P[b][2 * t][0], P[b][2 * t][1], P[b][2 * t + 1][0],
+                                                                P[b][2 * t + 1][1]));
+                        if constexpr (CAREFUL) {
+                            const Apart a = take_apart(v);
+                            const bf16x8_t one = as_bf16x8(make_uint4(seen[b][2 * t][0], seen[b][2 * t][1],
+                                                                      seen[b][2 * t + 1][0], seen[b][2 * t + 1][1]));
+                            O[b][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.finite, w, O[b][h], 0, 0, 0);
+                            up[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.up, one, up[b], 0, 0, 0);
+                            down[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.down, one, down[b], 0, 0, 0);
+                        } else {
+                            O[b][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w, O[b][h], 0, 0, 0);
+                        }
+                    }
+                }
+                if constexpr (CAREFUL) {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) O[b][h][i] = with_counts(O[b][h][i], up[b][i], down[b][i]);
+                }
+            }
+        };
+        auto run = [&](auto careful) __attribute__((always_inline)) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                m[b] = -INFINITY;
+                l[b] = 0.0f;
+#pragma unroll
+                for (int h = 0; h < kCols; ++h) O[b][h] = f32x4_t{};
+            }
+            if (wave >= steps) return;
+            stage(wave, KA, vmA, goneA);
+            for (int32_t i = wave; i < steps; i += 2 * kAttendWaves) {
+                const int32_t next = i + kAttendWaves, after = i + 2 * kAttendWaves;
+                if (next < steps) stage(next, KB, vmB, goneB);
+                key_step(careful, i, KA, vmA, goneA);
+                if (next >= steps) break;
+                if (after < steps) stage(after, KA, vmA, goneA);
+                key_step(careful, next, KB, vmB, goneB);
+            }
+        };
+        run(std::false_type{});
+        bool odd = false;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int h = 0; h < kCols; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) odd |= !(fabsf(O[b][h][i]) < INFINITY);
+        if (__syncthreads_or(odd)) run(std::true_type{});
+
+        // the waves' rows joined in LDS (where V was), 16 at a time
+        const bool whole = count == bl.count;
+        const float v_scale = E4M3 ? cache.v_scale[st.head] : 1.0f;
+        float* part = whole ? nullptr : Part<M, HD>::at(ws, wg, st.block == 0);
+        f32x4_t* const pool = reinterpret_cast<f32x4_t*>(vA);
+        constexpr int kVec = HD / 4;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const float lsum = quarter_sum(l[b]);
+            if (g4 == 0) {
+                wm[wave][16 * b + n16] = m[b];
+                wl[wave][16 * b + n16] = lsum;
+            }
+            __syncthreads();  // V (or the rows before) is no longer read
+#pragma unroll
+            for (int h = 0; h < kCols; ++h)
+                pool[(wave * 16 + n16) * kVec + ((4 * h + g4) ^ n16)] = O[b][h];
+            __syncthreads();
+            for (int e = tid; e < 16 * kVec; e += kAttendThreads) {
+                const int r = e / kVec, c = e % kVec, row = 16 * b + r;
+                float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kAttendWaves; ++w) top = fmaxf(top, wm[w][row]);
+                f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int w = 0; w < kAttendWaves; ++w) {
+                    const float f = weight_of(wm[w][row], top);
+                    sum += wl[w][row] * f;
+                    o += pool[(w * 16 + r) * kVec + (c ^ r)] * f;
+                }
+                if (!whole) {
+                    if (c == 0) {
+                        part[row] = top;
+                        part[M + row] = sum;
+                    }
+                    *reinterpret_cast<f32x4_t*>(part + 2 * M + row * HD + 4 * c) = o;
+                } else if (row < u.n_rows) {
+                    const float inv = sum == 0.0f ? 0.0f : v_scale / sum;
+                    *reinterpret_cast<uint2*>(out_row(in, u, row, HD) + 4 * c) =
+                        make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+                    if (c == 0) store_lse(in, u, row, top, sum);
+                }
+            }
+        }
+        if (!whole) {
+            const int64_t begin = at - st.block;
+            join_parts<M, HD>(in, ws, u, static_cast<int32_t>(begin / share),
+                              static_cast<int32_t>((begin + bl.count - 1) / share), v_scale, &flag);
+        }
+        __syncthreads();  // before V is copied in again
+
+        at += count;
+        st.block = 0;
+        if (++st.head == cache.n_kv) {
+            st.head = 0;
+            if (at < end)
+                do ++st.req;
+                while (span_of(in, cache, st.req).n == 0);
+        }
+    }
+}
+
+// --------------------------------------------------------------------- launch
+
+namespace {
+
+// Rows of a unit: all rows that a request can have where those are few.
+int32_t unit_rows(int32_t n_q, int32_t max_q, const KvCacheIn& c) {
+    const int64_t rows = static_cast<int64_t>(max_q) * (n_q / c.n_kv);
+    return rows <= 16 ? 16 : rows <= 32 ? 32 : kTileRows;
+}
+// Workgroups of a launch: as many as the chip holds at a time.
+int32_t workgroups(const KvCacheIn& c) { return c.head_dim > 128 ? 256 : 512; }
+
+struct WsLayout {
+    size_t start, done, parts, bytes;
+};
+WsLayout ws_layout(int32_t rows, const KvCacheIn& c) {
+    const size_t n = static_cast<size_t>(workgroups(c));
+    WsLayout w;
+    w.start = 256;
+    w.done = w.start + n * sizeof(WorkStart);
+    w.parts = w.done + n * sizeof(int32_t);
+    w.bytes = w.parts + 2 * n * rows * static_cast<size_t>(c.head_dim + 2) * sizeof(float);
+    return w;
+}
+
+using AttendKernel = void (*)(AttendIn, KvCacheIn, AttendWs, int32_t);
+// Indexed by head_dim (64, 128, 256), type and form (16 rows, 32 rows, tiles).
+constexpr AttendKernel kKernels[3][2][3] = {
+    {{attend_row_kernel<64, false, 1>, attend_row_kernel<64, false, 2>, attend_tile_kernel<64, false>},
+     {attend_row_kernel<64, true, 1>, attend_row_kernel<64, true, 2>, attend_tile_kernel<64, true>}},
+    {{attend_row_kernel<128, false, 1>, attend_row_kernel<128, false, 2>, attend_tile_kernel<128, false>},
+     {attend_row_kernel<128, true, 1>, attend_row_kernel<128, true, 2>, attend_tile_kernel<128, true>}},
+    {{attend_row_kernel<256, false, 1>, attend_row_kernel<256, false, 2>, attend_tile_kernel<256, false>},
+     {attend_row_kernel<256, true, 1>, attend_row_kernel<256, true, 2>, attend_tile_kernel<256, true>}}};
+AttendKernel kernel_for(int32_t hd, bool e4m3, int32_t rows) {
+    return kKernels[hd == 64 ? 0 : hd == 128 ? 1 : 2][e4m3][rows == 16 ? 0 : rows == 32 ? 1 : 2];
+}
+
+}  // namespace
+
+size_t attend_workspace(int32_t n_q, int32_t max_q, const KvCacheIn& cache) {
+    return ws_layout(unit_rows(n_q, max_q, cache), cache).bytes;
+}
+
+hipError_t launch_attend(const AttendIn& in, const KvCacheIn& cache, bool e4m3, void* ws,
                          hipStream_t stream) {
-    const dim3 grid(cache.R_max, in.n_q, min(in.max_q, 256));
-    if (e4m3)
-        hipLaunchKernelGGL(attend_kernel<true>, grid, dim3(kWave), 0, stream, in, cache);
-    else
-        hipLaunchKernelGGL(attend_kernel<false>, grid, dim3(kWave), 0, stream, in, cache);
+    const int32_t rows = unit_rows(in.n_q, in.max_q, cache), n_wg = workgroups(cache);
+    const WsLayout w = ws_layout(rows, cache);
+    char* p = static_cast<char*>(ws);
+    const AttendWs aw{reinterpret_cast<PlanHead*>(p), reinterpret_cast<WorkStart*>(p + w.start),
+                      reinterpret_cast<int32_t*>(p + w.done), reinterpret_cast<float*>(p + w.parts)};
+    const int64_t most = (static_cast<int64_t>(in.max_q) * (in.n_q / cache.n_kv) + rows - 1) / rows;
+    hipLaunchKernelGGL(attend_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, in, cache, aw, rows,
+                       n_wg, rows == kTileRows ? 4 : 4, most > 4 ? 1 : 0);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel_for(cache.head_dim, e4m3, rows), dim3(n_wg), dim3(kAttendThreads), 0, stream,
+                       in, cache, aw, n_wg);
     return hipGetLastError();
 }
 
 void add_attend_kernels(std::vector<KernelInfo>& t) {
-    t.push_back(kernel_info(attend_kernel<true>));
-    t.push_back(kernel_info(attend_kernel<false>));
+    t.push_back(kernel_info(attend_plan_kernel));
+    for (const auto& width : kKernels)
+        for (const auto& type : width)
+            for (const AttendKernel k : type) t.push_back(kernel_info(k));
 }
 
 }  // namespace xmix
