@@ -301,45 +301,82 @@ __device__ __forceinline__ float quarter_sum(float v) {
     return half_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
-// A V^T operand taken apart: its finite values, and ones where a value is +inf
-// or NaN, and -inf or NaN.  A product with a masked key's weight (zero) must leave
-// nothing, which it does not where the value is not finite; rows that see the key
-// get their infinity by the counts.
-struct Apart {
-    bf16x8_t finite, up, down;
+// Values that are not finite.  A masked key's weight is zero, and zero times an
+// infinity or NaN is not nothing.  Where O comes out not finite, the unit is done
+// again with each V tile made finite in LDS first, and the columns' keys of +inf (or
+// NaN) and -inf (or NaN) kept as 64-bit masks; a row that sees such a key gets its
+// infinity from the masks.
+struct OddKeys {
+    uint64_t up, down;
 };
-__device__ __forceinline__ Apart take_apart(const bf16x8_t& v) {
-    const uint4 w4 = __builtin_bit_cast(uint4, v);
-    const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-    uint32_t f[4], u[4], d[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[i] = u[i] = d[i] = 0;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const uint32_t x = (w[i] >> (16 * e)) & 0xFFFFu;
-            const bool odd = (x & 0x7F80u) == 0x7F80u, nan = odd && (x & 0x7Fu);
-            f[i] |= (odd ? 0u : x) << (16 * e);
-            u[i] |= (odd && (nan || !(x & 0x8000u)) ? 0x3F80u : 0u) << (16 * e);
-            d[i] |= (odd && (nan || (x & 0x8000u)) ? 0x3F80u : 0u) << (16 * e);
-        }
+// Takes the odd values out of one piece (bf16, or e4m3, which has NaN alone) of the
+// tile at `piece`; `cols` are the masks of its columns, `key` the tile's key.
+template <bool E4M3>
+__device__ __forceinline__ void take_odd(uint4* piece, OddKeys* cols, int key) {
+    constexpr int n = E4M3 ? 16 : 8;
+    uint32_t* w = reinterpret_cast<uint32_t*>(piece);
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+        const int sh = E4M3 ? 8 * (i & 3) : 16 * (i & 1), at = E4M3 ? i >> 2 : i >> 1;
+        const uint32_t x = (w[at] >> sh) & (E4M3 ? 0xFFu : 0xFFFFu);
+        const bool odd = E4M3 ? (x & 0x7Fu) == 0x7Fu : (x & 0x7F80u) == 0x7F80u;
+        if (!odd) continue;
+        const bool nan = E4M3 || (x & 0x7Fu);
+        w[at] &= ~((E4M3 ? 0xFFu : 0xFFFFu) << sh);
+        if (nan || !(x & 0x8000u)) atomicOr(reinterpret_cast<unsigned long long*>(&cols[i].up), 1ull << key);
+        if (nan || (x & 0x8000u)) atomicOr(reinterpret_cast<unsigned long long*>(&cols[i].down), 1ull << key);
     }
-    return {as_bf16x8(make_uint4(f[0], f[1], f[2], f[3])), as_bf16x8(make_uint4(u[0], u[1], u[2], u[3])),
-            as_bf16x8(make_uint4(d[0], d[1], d[2], d[3]))};
 }
-__device__ __forceinline__ float with_counts(float o, float up, float down) {
-    return o + (up > 0.0f ? INFINITY : 0.0f) + (down > 0.0f ? -INFINITY : 0.0f);
+__device__ __forceinline__ float with_odd(float o, const OddKeys& k, uint64_t see) {
+    if (k.up & see) o += INFINITY;
+    if (k.down & see) o -= INFINITY;
+    return o;
+}
+// The keys of a block of n (at most 64) from key0 on that a row sees.
+__device__ __forceinline__ uint64_t seen_keys(int32_t key0, int32_t pos, int32_t window, uint32_t gone) {
+    uint64_t see = pos < key0 ? 0 : pos - key0 >= 63 ? ~0ull : (2ull << (pos - key0)) - 1;
+    if (window > 0 && pos - window >= key0) {
+        const int32_t hidden = pos - window - key0;  // the last hidden one
+        see = hidden >= 63 ? 0 : see & ~((2ull << hidden) - 1);
+    }
+    for (int g = 0; g < kBlockKeys / kGroupKeys; ++g)
+        if ((gone >> g) & 1u) see &= ~(0xFFFFull << (kGroupKeys * g));
+    return see;
 }
 
 // ------------------------------------------------------------- joining parts
 
+constexpr int kThrough = 16;  // the sc1 bit of a buffer access: past the XCD's L2
+__device__ __forceinline__ void store_through(__amdgpu_buffer_rsrc_t r, int off, float v) {
+    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r, off, 0, kThrough);
+}
+__device__ __forceinline__ void store_through(__amdgpu_buffer_rsrc_t r, int off, const f32x4_t& v) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), r, off, 0, kThrough);
+}
+__device__ __forceinline__ float load_through(__amdgpu_buffer_rsrc_t r, int off) {
+    return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, off, 0, kThrough));
+}
+__device__ __forceinline__ f32x4_t load4_through(__amdgpu_buffer_rsrc_t r, int off) {
+    return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, kThrough));
+}
+
 // A part: the rows' maxima (powers of two, -inf: no key) and sums, then O [row][HD].
+// Parts pass between XCDs, whose L2 caches do not see each other's writes: they are
+// stored through to memory and loaded from there (sc1), which needs no fence.  An
+// agent fence writes the whole L2 back, a good half microsecond each, one
+// after the other: a call of 32 workgroups took 33 us with them and 10 without.
 template <int M, int HD>
 struct Part {
     static constexpr int kFloats = M * (HD + 2);
-    static __device__ float* at(const AttendWs& ws, int32_t wg, bool opens) {
-        return ws.parts + (2 * static_cast<int64_t>(wg) + (opens ? 1 : 0)) * kFloats;
+    __amdgpu_buffer_rsrc_t r;
+    __device__ __forceinline__ Part(const AttendWs& ws, int32_t wg, bool opens) {
+        float* p = ws.parts + (2 * static_cast<int64_t>(wg) + (opens ? 1 : 0)) * kFloats;
+        r = __builtin_amdgcn_make_buffer_rsrc(p, 0, kFloats * 4, kBufferDword3);
     }
+    __device__ __forceinline__ void put(int at, float v) const { store_through(r, at * 4, v); }
+    __device__ __forceinline__ void put4(int at, const f32x4_t& v) const { store_through(r, at * 4, v); }
+    __device__ __forceinline__ float get(int at) const { return load_through(r, at * 4); }
+    __device__ __forceinline__ f32x4_t get4(int at) const { return load4_through(r, at * 4); }
 };
 
 // The rows of a unit in the caller's tensors.
@@ -367,26 +404,39 @@ __device__ __forceinline__ float weight_of(float m, float top) {
 template <int M, int HD>
 __device__ void join_parts(const AttendIn& in, const AttendWs& ws, const RowsOut& u, int32_t first,
                            int32_t last, float v_scale, int* flag) {
-    __threadfence();
+    __builtin_amdgcn_s_waitcnt(0);  // this wave's stores have reached memory
     __syncthreads();
-    if (threadIdx.x == 0) *flag = atomicAdd(ws.done + first, 1) == last - first;
+    if (threadIdx.x == 0)
+        *flag = __hip_atomic_fetch_add(ws.done + first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+                last - first;
     __syncthreads();
     if (!*flag) return;
-    __threadfence();
-    constexpr int kVec = HD / 4;
+    constexpr int kVec = HD / 4, kAhead = 8;
     const int32_t rows = min(M, u.n_rows - u.row0);
     for (int32_t e = threadIdx.x; e < rows * kVec; e += kAttendThreads) {
         const int32_t row = e / kVec, c = e % kVec;
         float top = -INFINITY, l = 0.0f;
         f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int32_t w = first; w <= last; ++w) {
-            const float* p = Part<M, HD>::at(ws, w, w == first);
-            const float m = p[row], top2 = fmaxf(top, m);
-            const float a = weight_of(top, top2), b = weight_of(m, top2);
-            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(p + 2 * M + row * HD + 4 * c);
-            l = l * a + p[M + row] * b;
-            o = o * a + x * b;
-            top = top2;
+        for (int32_t w0 = first; w0 <= last; w0 += kAhead) {
+            float m[kAhead], s[kAhead];
+            f32x4_t x[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int32_t w = min(w0 + i, last);
+                const Part<M, HD> p(ws, w, w == first);
+                m[i] = p.get(row);
+                s[i] = p.get(M + row);
+                x[i] = p.get4(2 * M + row * HD + 4 * c);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (w0 + i > last) break;
+                const float top2 = fmaxf(top, m[i]);
+                const float a = weight_of(top, top2), b = weight_of(m[i], top2);
+                l = l * a + s[i] * b;
+                o = o * a + x[i] * b;
+                top = top2;
+            }
         }
         const float inv = l == 0.0f ? 0.0f : v_scale / l;
         *reinterpret_cast<uint2*>(out_row(in, u, row, HD) + 4 * c) =
@@ -412,6 +462,7 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
     constexpr int kCopies = kGroupKeys * RB / 1024;
     constexpr int kSteps = HD / 16, kCols = HD / 32;
     __shared__ uint4 kA[kTile], kB[kTile], vA[kTile], vB[kTile];
+    __shared__ OddKeys odd_keys[HD];
     __shared__ int flag;
     const int32_t wg = range_of_block(n_wg);
     const int64_t share = ws.head->share, blocks = ws.head->blocks;
@@ -476,12 +527,19 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
 
         float m, l;
         f32x16_t O[kCols];
-        // One block: scores, weights, O.  CAREFUL: values that are not finite may stand
-        // in masked places.
-        auto block_step = [&](auto careful, int32_t block, const uint4* kt, const uint4* vt)
-            __attribute__((always_inline)) {
-            constexpr bool CAREFUL = decltype(careful)::value;
+        bool careful = false;
+        // One block: scores, weights, O.
+        auto block_step = [&](int32_t block, const uint4* kt, uint4* vt) __attribute__((always_inline)) {
             const int32_t key0 = block * kBlockKeys;
+            if (careful) {
+                for (int c = tid; c < HD; c += kAttendThreads) odd_keys[c] = OddKeys{0, 0};
+                __syncthreads();
+                for (int e = tid; e < kTile; e += kAttendThreads) {
+                    const int kr = e / (RB / 16), slot = (e % (RB / 16)) ^ swz_v_tile<RB, E4M3>(kr);
+                    take_odd<E4M3>(vt + e, odd_keys + slot * (E4M3 ? 16 : 8), kr);
+                }
+                __syncthreads();
+            }
             if (!wave_on || key0 > p_last) return;
             f32x16_t S[2];
 #pragma unroll
@@ -540,7 +598,6 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
             }
             const float off = m == -INFINITY ? 0.0f : m;
             uint32_t P[2][8];
-            uint32_t seen[CAREFUL ? 2 : 1][8];
             float sum = 0.0f;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
@@ -551,14 +608,10 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                     sum += x;
                     sum += y;
                     P[b][i / 2] = weights2(x, y);
-                    if constexpr (CAREFUL)
-                        seen[b][i / 2] = (S[b][i] == -INFINITY ? 0u : 0x3F80u) |
-                                         (S[b][i + 1] == -INFINITY ? 0u : 0x3F800000u);
                 }
             l += sum;
 #pragma unroll
             for (int h = 0; h < kCols; ++h) {
-                f32x16_t up = {}, down = {};
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     const int b = t / 2, i0 = 4 * (t % 2);
@@ -583,23 +636,19 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                         }
                         v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
                     }
-                    if constexpr (CAREFUL) {
-                        const Apart a = take_apart(v);
-                        const bf16x8_t one = as_bf16x8(make_uint4(seen[b][i0], seen[b][i0 + 1], seen[b][i0 + 2], seen[b][i0 + 3]));
-                        O[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.finite, w, O[h], 0, 0, 0);
-                        up = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.up, one, up, 0, 0, 0);
-                        down = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.down, one, down, 0, 0, 0);
-                    } else {
-                        O[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, O[h], 0, 0, 0);
-                    }
-                }
-                if constexpr (CAREFUL) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) O[h][i] = with_counts(O[h][i], up[i], down[i]);
+                    O[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, O[h], 0, 0, 0);
                 }
             }
+            if (careful) {
+                const uint64_t see = seen_keys(key0, pos, in.window, gone);
+#pragma unroll
+                for (int h = 0; h < kCols; ++h)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        O[h][i] = with_odd(O[h][i], odd_keys[32 * h + 8 * (i / 4) + 4 * half + i % 4], see);
+            }
         };
-        auto run = [&](auto careful) __attribute__((always_inline)) {
+        for (;;) {
             m = -INFINITY;
             l = 0.0f;
 #pragma unroll
@@ -611,21 +660,21 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                 __builtin_amdgcn_s_waitcnt(0);
                 __syncthreads();
                 if (i + 1 < count) stage(b0 + i + 1, kB, vB);
-                block_step(careful, b0 + i, kA, vA);
+                block_step(b0 + i, kA, vA);
                 if (i + 1 >= count) break;
                 __builtin_amdgcn_s_waitcnt(0);
                 __syncthreads();
                 if (i + 2 < count) stage(b0 + i + 2, kA, vA);
-                block_step(careful, b0 + i + 1, kB, vB);
+                block_step(b0 + i + 1, kB, vB);
             }
-        };
-        run(std::false_type{});
-        bool odd = false;
+            bool odd = false;
 #pragma unroll
-        for (int h = 0; h < kCols; ++h)
+            for (int h = 0; h < kCols; ++h)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) odd |= !(fabsf(O[h][i]) < INFINITY);
-        if (__syncthreads_or(odd)) run(std::true_type{});
+                for (int i = 0; i < 16; ++i) odd |= !(fabsf(O[h][i]) < INFINITY);
+            if (careful || !__syncthreads_or(odd)) break;
+            careful = true;
+        }
         l = half_sum(l);
 
         if (count == bl.count) {
@@ -642,18 +691,18 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                 if (half == 0) store_lse(in, u, wave * 32 + n32, m, l);
             }
         } else {
-            float* part = Part<kTileRows, HD>::at(ws, wg, st.block == 0);
+            const Part<kTileRows, HD> part(ws, wg, st.block == 0);
             const int r = wave * 32 + n32;
             if (half == 0) {
-                part[r] = m;
-                part[kTileRows + r] = l;
+                part.put(r, m);
+                part.put(kTileRows + r, l);
             }
 #pragma unroll
             for (int h = 0; h < kCols; ++h)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4)
-                    *reinterpret_cast<f32x4_t*>(part + 2 * kTileRows + r * HD + 32 * h + 2 * i + 4 * half) =
-                        f32x4_t{O[h][i], O[h][i + 1], O[h][i + 2], O[h][i + 3]};
+                    part.put4(2 * kTileRows + r * HD + 32 * h + 2 * i + 4 * half,
+                              f32x4_t{O[h][i], O[h][i + 1], O[h][i + 2], O[h][i + 3]});
             const int64_t begin = at - st.block;
             join_parts<kTileRows, HD>(in, ws, u, static_cast<int32_t>(begin / share),
                                       static_cast<int32_t>((begin + bl.count - 1) / share),
@@ -689,6 +738,7 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
     static_assert(kAttendWaves * kTile >= kAttendWaves * 16 * HD / 4, "room to join the waves");
     __shared__ uint4 vA[kAttendWaves * kTile], vB[kAttendWaves * kTile];
     __shared__ float wm[kAttendWaves][M], wl[kAttendWaves][M];
+    __shared__ OddKeys odd_keys[kAttendWaves][HD];
     __shared__ int flag;
     const int32_t wg = range_of_block(n_wg);
     const int64_t share = ws.head->share, blocks = ws.head->blocks;
@@ -766,10 +816,19 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
 
         float m[NB], l[NB];
         f32x4_t O[NB][kCols];
-        auto key_step = [&](auto careful, int32_t step, const uint4 (&K)[kGroups][kLoads], const uint4* vt,
-                            uint32_t gone) __attribute__((always_inline)) {
-            constexpr bool CAREFUL = decltype(careful)::value;
+        bool careful = false;
+        auto key_step = [&](int32_t step, const uint4 (&K)[kGroups][kLoads], uint4* vt, uint32_t gone)
+            __attribute__((always_inline)) {
             const int32_t key0 = key_from + step * KS;
+            if (careful) {  // the tile and the masks are this wave's own
+                for (int c = lane; c < HD; c += kWave) odd_keys[wave][c] = OddKeys{0, 0};
+                __builtin_amdgcn_s_waitcnt(0);
+                for (int e = lane; e < kTile; e += kWave) {
+                    const int kr = e / (RB / 16), slot = (e % (RB / 16)) ^ swz_v_row<RB, E4M3>(kr);
+                    take_odd<E4M3>(vt + e, odd_keys[wave] + slot * (E4M3 ? 16 : 8), kr);
+                }
+                __builtin_amdgcn_s_waitcnt(0);
+            }
             f32x4_t S[NB][kGroups];
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
@@ -803,7 +862,7 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                         }
                 }
             }
-            uint32_t P[NB][kGroups][2], seen[CAREFUL ? NB : 1][kGroups][2];
+            uint32_t P[NB][kGroups][2];
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 float top = S[b][0][0];
@@ -828,16 +887,12 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                         const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(S[b][g][2 * i + 1], c2, -off));
                         l[b] += x + y;
                         P[b][g][i] = weights2(x, y);
-                        if constexpr (CAREFUL)
-                            seen[b][g][i] = (S[b][g][2 * i] == -INFINITY ? 0u : 0x3F80u) |
-                                            (S[b][g][2 * i + 1] == -INFINITY ? 0u : 0x3F800000u);
                     }
             }
 #pragma unroll
             for (int h = 0; h < kCols; ++h) {
-                f32x4_t up[NB], down[NB];
-#pragma unroll
-                for (int b = 0; b < NB; ++b) up[b] = down[b] = f32x4_t{};
+                // (few operands of V in flight: more cost registers that are not there)
+                if (h % 4 == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int t = 0; t < kGroups / 2; ++t) {
                     bf16x8_t v;
@@ -863,27 +918,23 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                     for (int b = 0; b < NB; ++b) {
                         const bf16x8_t w = as_bf16x8(make_uint4(P[b][2 * t][0], P[b][2 * t][1], P[b][2 * t + 1][0],
                                                                 P[b][2 * t + 1][1]));
-                        if constexpr (CAREFUL) {
-                            const Apart a = take_apart(v);
-                            const bf16x8_t one = as_bf16x8(make_uint4(seen[b][2 * t][0], seen[b][2 * t][1],
-                                                                      seen[b][2 * t + 1][0], seen[b][2 * t + 1][1]));
-                            O[b][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.finite, w, O[b][h], 0, 0, 0);
-                            up[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.up, one, up[b], 0, 0, 0);
-                            down[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.down, one, down[b], 0, 0, 0);
-                        } else {
-                            O[b][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w, O[b][h], 0, 0, 0);
-                        }
+                        O[b][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w, O[b][h], 0, 0, 0);
                     }
                 }
-                if constexpr (CAREFUL) {
+            }
+            if (careful) {
 #pragma unroll
-                    for (int b = 0; b < NB; ++b)
+                for (int b = 0; b < NB; ++b) {
+                    const uint64_t see = seen_keys(key0, pos[b], in.window, gone);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) O[b][h][i] = with_counts(O[b][h][i], up[b][i], down[b][i]);
+                    for (int h = 0; h < kCols; ++h)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            O[b][h][i] = with_odd(O[b][h][i], odd_keys[wave][16 * h + 4 * g4 + i], see);
                 }
             }
         };
-        auto run = [&](auto careful) __attribute__((always_inline)) {
+        for (;;) {
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 m[b] = -INFINITY;
@@ -891,31 +942,30 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
 #pragma unroll
                 for (int h = 0; h < kCols; ++h) O[b][h] = f32x4_t{};
             }
-            if (wave >= steps) return;
-            stage(wave, KA, vmA, goneA);
+            if (wave < steps) stage(wave, KA, vmA, goneA);
             for (int32_t i = wave; i < steps; i += 2 * kAttendWaves) {
                 const int32_t next = i + kAttendWaves, after = i + 2 * kAttendWaves;
                 if (next < steps) stage(next, KB, vmB, goneB);
-                key_step(careful, i, KA, vmA, goneA);
+                key_step(i, KA, vmA, goneA);
                 if (next >= steps) break;
                 if (after < steps) stage(after, KA, vmA, goneA);
-                key_step(careful, next, KB, vmB, goneB);
+                key_step(next, KB, vmB, goneB);
             }
-        };
-        run(std::false_type{});
-        bool odd = false;
+            bool odd = false;
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int h = 0; h < kCols; ++h)
+                for (int h = 0; h < kCols; ++h)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) odd |= !(fabsf(O[b][h][i]) < INFINITY);
-        if (__syncthreads_or(odd)) run(std::true_type{});
+                    for (int i = 0; i < 4; ++i) odd |= !(fabsf(O[b][h][i]) < INFINITY);
+            if (careful || !__syncthreads_or(odd)) break;
+            careful = true;
+        }
 
         // the waves' rows joined in LDS (where V was), 16 at a time
         const bool whole = count == bl.count;
         const float v_scale = E4M3 ? cache.v_scale[st.head] : 1.0f;
-        float* part = whole ? nullptr : Part<M, HD>::at(ws, wg, st.block == 0);
+        const Part<M, HD> part(ws, wg, st.block == 0);
         f32x4_t* const pool = reinterpret_cast<f32x4_t*>(vA);
         constexpr int kVec = HD / 4;
 #pragma unroll
@@ -944,10 +994,10 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                 }
                 if (!whole) {
                     if (c == 0) {
-                        part[row] = top;
-                        part[M + row] = sum;
+                        part.put(row, top);
+                        part.put(M + row, sum);
                     }
-                    *reinterpret_cast<f32x4_t*>(part + 2 * M + row * HD + 4 * c) = o;
+                    part.put4(2 * M + row * HD + 4 * c, o);
                 } else if (row < u.n_rows) {
                     const float inv = sum == 0.0f ? 0.0f : v_scale / sum;
                     *reinterpret_cast<uint2*>(out_row(in, u, row, HD) + 4 * c) =
