@@ -83,13 +83,20 @@ struct ArgPointers<AttendWs> {
 
 // ------------------------------------------------------------------- geometry
 
+// A value that nothing writes during the launch, at a uniform place: a scalar load,
+// which waits for no vector load before it (a page id behind the copies of the
+// block before would wait for all of them).
+template <typename T>
+__device__ __forceinline__ T scalar_load(const T* p) {
+    return *(const __attribute__((address_space(4))) T*)reinterpret_cast<uintptr_t>(p);
+}
+
 // A request's span and keys; n = 0 where it has no rows to write.
 struct Span {
     int32_t lo, n, len;
 };
-__device__ __forceinline__ Span span_of(const AttendIn& in, const KvCacheIn& c, int32_t r,
-                                        bool* bad = nullptr) {
-    const int32_t lo = in.cu[r], hi = in.cu[r + 1], len = in.kv_len[r];
+__device__ __forceinline__ Span span_of(const AttendIn& in, const KvCacheIn& c, int32_t lo, int32_t hi,
+                                        int32_t len, bool* bad = nullptr) {
     Span s{lo, 0, len};
     if (lo < 0 || hi < lo || hi > in.T_max) {
         if (bad) *bad = true;
@@ -103,6 +110,16 @@ __device__ __forceinline__ Span span_of(const AttendIn& in, const KvCacheIn& c, 
     s.n = hi - lo;
     return s;
 }
+__device__ __forceinline__ Span span_of(const AttendIn& in, const KvCacheIn& c, int32_t r, bool* bad = nullptr) {
+    return span_of(in, c, in.cu[r], in.cu[r + 1], in.kv_len[r], bad);
+}
+// The same of a uniform request.
+__device__ __forceinline__ Span scalar_span(const AttendIn& in, const KvCacheIn& c, int32_t r) {
+    return span_of(in, c, scalar_load(in.cu + r), scalar_load(in.cu + r + 1), scalar_load(in.kv_len + r));
+}
+// A uniform value in a scalar register, where the compiler has put it in a vector one
+// (a resource made of it would be rebuilt lane by lane).
+__device__ __forceinline__ int32_t scalar(int32_t v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ int32_t tiles_of(int32_t n, int32_t group, int32_t rows) {
     return static_cast<int32_t>((static_cast<int64_t>(n) * group + rows - 1) / rows);
 }
@@ -246,7 +263,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t group_rows(const void* base, c
                                                              int32_t key, int32_t len) {
     const bool ok = page_ok(c, page);
     const int64_t row = page_row(c, ok ? page : 0, head, key & ((1 << c.page_log2) - 1));
-    const int32_t live = ok ? max(0, min(kGroupKeys, len - key)) : 0;
+    const int32_t live = scalar(ok ? max(0, min(kGroupKeys, len - key)) : 0);
     return __builtin_amdgcn_make_buffer_rsrc(
         const_cast<char*>(static_cast<const char*>(base)) + row * RB, 0, live * RB, kBufferDword3);
 }
@@ -254,7 +271,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t group_rows(const void* base, c
 __device__ __forceinline__ int32_t page_of_key(const KvCacheIn& c, int32_t req, int32_t key,
                                                int32_t len) {
     const int32_t nth = max(0, min(key, len - 1)) >> c.page_log2;
-    return __builtin_amdgcn_readfirstlane(page_at(c, req, nth));
+    return scalar_load(c.pages + static_cast<int64_t>(req) * c.max_pages + nth);
 }
 
 typedef __attribute__((address_space(3))) void* lds_ptr;
@@ -262,8 +279,16 @@ typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4;
 typedef __attribute__((address_space(3))) i32x2_t* lds_i32x2;
 
 // Sixteen bytes per lane from `off` bytes into the resource to dst (uniform) + lane.
+constexpr int kOnce = 2;  // the nt bit of a buffer access: bytes that nobody reads again
+template <int AUX = 0>
 __device__ __forceinline__ void copy16(__amdgpu_buffer_rsrc_t r, uint4* dst, int32_t off) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)dst, 16, off, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)dst, 16, off, 0, 0, AUX);
+}
+// Waits until at most n of this wave's vector loads and copies are outstanding.
+template <int n>
+__device__ __forceinline__ void wait_all_but() {
+    __builtin_amdgcn_s_waitcnt((n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14));
+    asm volatile("" ::: "memory");
 }
 __device__ __forceinline__ bf16x8_t as_bf16x8(const uint4& v) {
     return __builtin_bit_cast(bf16x8_t, v);
@@ -410,7 +435,7 @@ __device__ void join_parts(const AttendIn& in, const AttendWs& ws, const RowsOut
         *flag = __hip_atomic_fetch_add(ws.done + first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
                 last - first;
     __syncthreads();
-    if (!*flag) return;
+    if (!scalar(*flag)) return;
     constexpr int kVec = HD / 4, kAhead = 8;
     const int32_t rows = min(M, u.n_rows - u.row0);
     for (int32_t e = threadIdx.x; e < rows * kVec; e += kAttendThreads) {
@@ -465,14 +490,15 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
     __shared__ OddKeys odd_keys[HD];
     __shared__ int flag;
     const int32_t wg = range_of_block(n_wg);
-    const int64_t share = ws.head->share, blocks = ws.head->blocks;
+    const int64_t share = scalar_load(&ws.head->share), blocks = scalar_load(&ws.head->blocks);
     int64_t at = wg * share;
     const int64_t end = min(at + share, blocks);
     if (at >= end) return;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, n32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int32_t group = in.n_q / cache.n_kv;
-    WorkStart st = ws.start[wg];
+    WorkStart st{scalar_load(&ws.start[wg].req), scalar_load(&ws.start[wg].head),
+                 scalar_load(&ws.start[wg].tile), scalar_load(&ws.start[wg].block)};
 
     // this lane's sources within a group of 16 rows, and its reads of a block
     int32_t src_k[kCopies], src_v[kCopies];
@@ -484,12 +510,12 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
     }
 
     while (at < end) {
-        const Span s = span_of(in, cache, st.req);
+        const Span s = scalar_span(in, cache, st.req);
         const int32_t tiles = tiles_of(s.n, group, kTileRows);
         const Blocks bl = blocks_of(s, st.tile, group, kTileRows, in.window);
         const int32_t count = static_cast<int32_t>(min(static_cast<int64_t>(bl.count - st.block), end - at));
         const RowsOut u{s.lo, s.n * group, st.tile * kTileRows, st.head, group};
-        const float ks = E4M3 ? cache.k_scale[st.head] : 1.0f;
+        const float ks = E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f;
         const float c2 = in.scale * ks * kLog2e;
         // this lane's row, and the tokens of the wave's rows
         const int32_t row = u.row0 + wave * 32 + n32;
@@ -672,14 +698,14 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
             for (int h = 0; h < kCols; ++h)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) odd |= !(fabsf(O[h][i]) < INFINITY);
-            if (careful || !__syncthreads_or(odd)) break;
+            if (careful || !scalar(__syncthreads_or(odd))) break;
             careful = true;
         }
         l = half_sum(l);
 
         if (count == bl.count) {
             if (row_ok) {
-                const float inv = l == 0.0f ? 0.0f : (E4M3 ? cache.v_scale[st.head] : 1.0f) / l;
+                const float inv = l == 0.0f ? 0.0f : (E4M3 ? scalar_load(cache.v_scale + st.head) : 1.0f) / l;
                 uint16_t* out = out_row(in, u, wave * 32 + n32, HD);
 #pragma unroll
                 for (int h = 0; h < kCols; ++h)
@@ -706,7 +732,7 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
             const int64_t begin = at - st.block;
             join_parts<kTileRows, HD>(in, ws, u, static_cast<int32_t>(begin / share),
                                       static_cast<int32_t>((begin + bl.count - 1) / share),
-                                      E4M3 ? cache.v_scale[st.head] : 1.0f, &flag);
+                                      E4M3 ? scalar_load(cache.v_scale + st.head) : 1.0f, &flag);
         }
 
         at += count;
@@ -717,7 +743,7 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                 st.head = 0;
                 if (at < end)
                     do ++st.req;
-                    while (span_of(in, cache, st.req).n == 0);
+                    while (scalar_span(in, cache, st.req).n == 0);
             }
         }
     }
@@ -741,14 +767,15 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
     __shared__ OddKeys odd_keys[kAttendWaves][HD];
     __shared__ int flag;
     const int32_t wg = range_of_block(n_wg);
-    const int64_t share = ws.head->share, blocks = ws.head->blocks;
+    const int64_t share = scalar_load(&ws.head->share), blocks = scalar_load(&ws.head->blocks);
     int64_t at = wg * share;
     const int64_t end = min(at + share, blocks);
     if (at >= end) return;
     const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, n16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int32_t group = in.n_q / cache.n_kv;
-    WorkStart st = ws.start[wg];
+    WorkStart st{scalar_load(&ws.start[wg].req), scalar_load(&ws.start[wg].head),
+                 scalar_load(&ws.start[wg].tile), scalar_load(&ws.start[wg].block)};
 
     // sources of V's copies, by their place in the step; swz_v_row takes the row's
     // bits up to 4, so groups of 16 rows come in two kinds
@@ -764,11 +791,11 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
     uint4* const vmB = vB + wave * kTile;
 
     while (at < end) {
-        const Span s = span_of(in, cache, st.req);
+        const Span s = scalar_span(in, cache, st.req);
         const Blocks bl = blocks_of(s, 0, group, M, in.window);
         const int32_t count = static_cast<int32_t>(min(static_cast<int64_t>(bl.count - st.block), end - at));
         const RowsOut u{s.lo, s.n * group, 0, st.head, group};
-        const float c2 = in.scale * (E4M3 ? cache.k_scale[st.head] : 1.0f) * kLog2e;
+        const float c2 = in.scale * (E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f) * kLog2e;
         const int32_t base = s.len - s.n;
         const int32_t p_first = base, p_last = s.len - 1;
         int32_t pos[NB];
@@ -791,27 +818,33 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
 
         uint4 KA[kGroups][kLoads], KB[kGroups][kLoads];
         uint32_t goneA, goneB;
+        // Every step of the pipeline issues its loads, past the last one of nothing
+        // (resources without rows): with a branch around them the wait for one step's
+        // K would be for everything outstanding.
         auto stage = [&](int32_t step, uint4 (&K)[kGroups][kLoads], uint4* vd, uint32_t& gone)
             __attribute__((always_inline)) {
-            const int32_t key0 = key_from + step * KS;
+            const int32_t key0 = key_from + step * KS, len = step < steps ? s.len : 0;
+            __amdgpu_buffer_rsrc_t vr[kGroups];
             gone = 0;
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
                 const int32_t key = key0 + g * kGroupKeys;
-                const int32_t page = page_of_key(cache, st.req, key, s.len);
+                const int32_t page = page_of_key(cache, st.req, key, len);
                 if (!page_ok(cache, page)) gone |= 1u << g;
-                const __amdgpu_buffer_rsrc_t kr = group_rows<RB>(cache.k, cache, page, st.head, key, s.len);
-                const __amdgpu_buffer_rsrc_t vr = group_rows<RB>(cache.v, cache, page, st.head, key, s.len);
+                const __amdgpu_buffer_rsrc_t kr = group_rows<RB>(cache.k, cache, page, st.head, key, len);
+                vr[g] = group_rows<RB>(cache.v, cache, page, st.head, key, len);
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) {
                     const u32x4_t w = __builtin_bit_cast(
-                        u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(kr, n16 * RB + (4 * i + g4) * 16, 0, 0));
+                        u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(kr, n16 * RB + (4 * i + g4) * 16, 0, kOnce));
                     K[g][i] = make_uint4(w.x, w.y, w.z, w.w);
                 }
+            }
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g)
 #pragma unroll
                 for (int i = 0; i < kCopies; ++i)
-                    copy16(vr, vd + g * (kGroupKeys * RB / 16) + i * 64, src_v[g & 1][i]);
-            }
+                    copy16<kOnce>(vr[g], vd + g * (kGroupKeys * RB / 16) + i * 64, src_v[g & 1][i]);
         };
 
         float m[NB], l[NB];
@@ -889,10 +922,9 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                         P[b][g][i] = weights2(x, y);
                     }
             }
+            wait_all_but<kGroups * (kLoads + kCopies)>();  // the next step's loads: V is there
 #pragma unroll
             for (int h = 0; h < kCols; ++h) {
-                // (few operands of V in flight: more cost registers that are not there)
-                if (h % 4 == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int t = 0; t < kGroups / 2; ++t) {
                     bf16x8_t v;
@@ -942,14 +974,12 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
 #pragma unroll
                 for (int h = 0; h < kCols; ++h) O[b][h] = f32x4_t{};
             }
-            if (wave < steps) stage(wave, KA, vmA, goneA);
+            stage(wave, KA, vmA, goneA);
             for (int32_t i = wave; i < steps; i += 2 * kAttendWaves) {
-                const int32_t next = i + kAttendWaves, after = i + 2 * kAttendWaves;
-                if (next < steps) stage(next, KB, vmB, goneB);
+                stage(i + kAttendWaves, KB, vmB, goneB);
                 key_step(i, KA, vmA, goneA);
-                if (next >= steps) break;
-                if (after < steps) stage(after, KA, vmA, goneA);
-                key_step(next, KB, vmB, goneB);
+                stage(i + 2 * kAttendWaves, KA, vmA, goneA);
+                if (i + kAttendWaves < steps) key_step(i + kAttendWaves, KB, vmB, goneB);
             }
             bool odd = false;
 #pragma unroll
@@ -958,13 +988,13 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                 for (int h = 0; h < kCols; ++h)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) odd |= !(fabsf(O[b][h][i]) < INFINITY);
-            if (careful || !__syncthreads_or(odd)) break;
+            if (careful || !scalar(__syncthreads_or(odd))) break;
             careful = true;
         }
 
         // the waves' rows joined in LDS (where V was), 16 at a time
         const bool whole = count == bl.count;
-        const float v_scale = E4M3 ? cache.v_scale[st.head] : 1.0f;
+        const float v_scale = E4M3 ? scalar_load(cache.v_scale + st.head) : 1.0f;
         const Part<M, HD> part(ws, wg, st.block == 0);
         f32x4_t* const pool = reinterpret_cast<f32x4_t*>(vA);
         constexpr int kVec = HD / 4;
@@ -1019,7 +1049,7 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
             st.head = 0;
             if (at < end)
                 do ++st.req;
-                while (span_of(in, cache, st.req).n == 0);
+                while (scalar_span(in, cache, st.req).n == 0);
         }
     }
 }
