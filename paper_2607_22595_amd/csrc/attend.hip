@@ -274,6 +274,17 @@ __device__ __forceinline__ int32_t page_of_key(const KvCacheIn& c, int32_t req, 
     return scalar_load(c.pages + static_cast<int64_t>(req) * c.max_pages + nth);
 }
 
+// An offset that the compiler computes from here on anew: a tile's reads differ by an
+// exclusive or with a constant (the permutation of the pieces), one instruction each,
+// and kept apart would hold a register each through the whole loop.
+__device__ __forceinline__ int fresh(int off) {
+    asm volatile("" : "+v"(off));
+    return off;
+}
+__device__ __forceinline__ const uint4* at_bytes(const uint4* p, int off) {
+    return reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) + off);
+}
+
 typedef __attribute__((address_space(3))) void* lds_ptr;
 typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4;
 typedef __attribute__((address_space(3))) i32x2_t* lds_i32x2;
@@ -328,9 +339,9 @@ __device__ __forceinline__ float quarter_sum(float v) {
 
 // Values that are not finite.  A masked key's weight is zero, and zero times an
 // infinity or NaN is not nothing.  Where O comes out not finite, the unit is done
-// again with each V tile made finite in LDS first, and the columns' keys of +inf (or
-// NaN) and -inf (or NaN) kept as 64-bit masks; a row that sees such a key gets its
-// infinity from the masks.
+// again ("careful"): each V tile is made finite in LDS first, its columns' keys of
+// +inf (or NaN) and -inf (or NaN) go into 64-bit masks, and each row that sees one of
+// them notes the column; the notes become infinities when the rows are stored.
 struct OddKeys {
     uint64_t up, down;
 };
@@ -352,11 +363,26 @@ __device__ __forceinline__ void take_odd(uint4* piece, OddKeys* cols, int key) {
         if (nan || (x & 0x8000u)) atomicOr(reinterpret_cast<unsigned long long*>(&cols[i].down), 1ull << key);
     }
 }
-__device__ __forceinline__ float with_odd(float o, const OddKeys& k, uint64_t see) {
-    if (k.up & see) o += INFINITY;
-    if (k.down & see) o -= INFINITY;
-    return o;
-}
+// The notes of a unit's rows: a bit per column, of the two kinds.
+template <int M, int HD>
+struct OddNotes {
+    uint32_t bits[2][M][HD / 32];
+    __device__ __forceinline__ void clear(int tid) {
+        uint32_t* w = &bits[0][0][0];
+        for (int i = tid; i < 2 * M * HD / 32; i += kAttendThreads) w[i] = 0;
+    }
+    // Row `row` sees the keys `see` of the tile whose columns' masks are `cols`.
+    __device__ __forceinline__ void note(int kind, int row, uint64_t see, const OddKeys* cols) {
+#pragma unroll 1
+        for (int c = 0; c < HD; ++c)
+            if ((kind ? cols[c].down : cols[c].up) & see) atomicOr(&bits[kind][row][c / 32], 1u << (c % 32));
+    }
+    __device__ __forceinline__ float apply(float o, int row, int c) const {
+        if ((bits[0][row][c / 32] >> (c % 32)) & 1u) o += INFINITY;
+        if ((bits[1][row][c / 32] >> (c % 32)) & 1u) o -= INFINITY;
+        return o;
+    }
+};
 // The keys of a block of n (at most 64) from key0 on that a row sees.
 __device__ __forceinline__ uint64_t seen_keys(int32_t key0, int32_t pos, int32_t window, uint32_t gone) {
     uint64_t see = pos < key0 ? 0 : pos - key0 >= 63 ? ~0ull : (2ull << (pos - key0)) - 1;
@@ -488,6 +514,7 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
     constexpr int kSteps = HD / 16, kCols = HD / 32;
     __shared__ uint4 kA[kTile], kB[kTile], vA[kTile], vB[kTile];
     __shared__ OddKeys odd_keys[HD];
+    __shared__ OddNotes<kTileRows, HD> notes;
     __shared__ int flag;
     const int32_t wg = range_of_block(n_wg);
     const int64_t share = scalar_load(&ws.head->share), blocks = scalar_load(&ws.head->blocks);
@@ -508,6 +535,12 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
         src_k[i] = row * RB + ((slot ^ swz_k<RB>(row)) * 16);
         src_v[i] = row * RB + ((slot ^ swz_v_tile<RB, E4M3>(row)) * 16);
     }
+    // K: piece 2 i + half of row n32.  V: column block h of four (bf16) or eight keys.
+    const int i16 = lane & 15, side = (lane >> 4) & 1;
+    const int k_off = n32 * RB + ((half ^ swz_k<RB>(n32)) * 16);
+    const int v_row = E4M3 ? 8 * (i16 >> 3) + 4 * half + ((i16 >> 1) & 3) : 4 * half + (i16 >> 2);
+    const int v_piece = E4M3 ? side : 2 * side + ((i16 & 3) >> 1);
+    const int v_off = v_row * RB + ((v_piece ^ swz_v_tile<RB, E4M3>(v_row)) * 16) + 8 * (i16 & 1);
 
     while (at < end) {
         const Span s = scalar_span(in, cache, st.req);
@@ -557,6 +590,12 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
         // One block: scores, weights, O.
         auto block_step = [&](int32_t block, const uint4* kt, uint4* vt) __attribute__((always_inline)) {
             const int32_t key0 = block * kBlockKeys;
+            // pages that are not there, by groups of 16 keys
+            uint32_t gone = 0;
+#pragma unroll
+            for (int g = 0; g < kBlockKeys / kGroupKeys; ++g)
+                if (!page_ok(cache, page_of_key(cache, st.req, key0 + g * kGroupKeys, s.len)))
+                    gone |= 1u << g;
             if (careful) {
                 for (int c = tid; c < HD; c += kAttendThreads) odd_keys[c] = OddKeys{0, 0};
                 __syncthreads();
@@ -565,35 +604,33 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                     take_odd<E4M3>(vt + e, odd_keys + slot * (E4M3 ? 16 : 8), kr);
                 }
                 __syncthreads();
+                const int r = tid % kTileRows;
+                notes.note(tid / kTileRows, r,
+                           seen_keys(key0, base + min(u.row0 + r, u.n_rows - 1) / group, in.window, gone),
+                           odd_keys);
             }
             if (!wave_on || key0 > p_last) return;
             f32x16_t S[2];
+            const int ko = fresh(k_off);
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 f32x16_t acc = {};
-                const int kr = 32 * b + n32;
-                const uint4* krow = kt + kr * (RB / 16);
+                const uint4* rows = kt + 32 * b * (RB / 16);
                 if constexpr (E4M3) {
 #pragma unroll
                     for (int i = 0; i < kSteps / 2; ++i) {
-                        const uint4 w = krow[(2 * i + half) ^ swz_k<RB>(kr)];
+                        const uint4 w = *at_bytes(rows, ko ^ (32 * i));
                         acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e4m3_to_bf16(w.x, w.y), Q[2 * i], acc, 0, 0, 0);
                         acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e4m3_to_bf16(w.z, w.w), Q[2 * i + 1], acc, 0, 0, 0);
                     }
                 } else {
 #pragma unroll
                     for (int i = 0; i < kSteps; ++i)
-                        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            as_bf16x8(krow[(2 * i + half) ^ swz_k<RB>(kr)]), Q[i], acc, 0, 0, 0);
+                        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*at_bytes(rows, ko ^ (32 * i))),
+                                                                      Q[i], acc, 0, 0, 0);
                 }
                 S[b] = acc;
             }
-            // pages that are not there, by groups of 16 keys
-            uint32_t gone = 0;
-#pragma unroll
-            for (int g = 0; g < kBlockKeys / kGroupKeys; ++g)
-                if (!page_ok(cache, page_of_key(cache, st.req, key0 + g * kGroupKeys, s.len)))
-                    gone |= 1u << g;
             if (gone || key0 + kBlockKeys - 1 > p_first ||
                 (in.window > 0 && key0 <= p_last - in.window)) {
                 if (gone && lane == 0 && key0 < s.len) atomicOr(in.err_word, kErrKvPage);
@@ -636,6 +673,7 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                     P[b][i / 2] = weights2(x, y);
                 }
             l += sum;
+            const int vo = fresh(v_off);
 #pragma unroll
             for (int h = 0; h < kCols; ++h) {
 #pragma unroll
@@ -643,35 +681,20 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                     const int b = t / 2, i0 = 4 * (t % 2);
                     const bf16x8_t w = as_bf16x8(make_uint4(P[b][i0], P[b][i0 + 1], P[b][i0 + 2], P[b][i0 + 3]));
                     bf16x8_t v;
-                    const int i16 = lane & 15, side = (lane >> 4) & 1;
                     if constexpr (E4M3) {
-                        const int r8 = i16 >> 1, kr = 16 * t + 8 * (r8 / 4) + 4 * half + r8 % 4;
-                        const uint4* p = vt + kr * (RB / 16) + ((2 * h + side) ^ swz_v_tile<RB, true>(kr));
                         const i32x2_t x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                            (lds_i32x2)(reinterpret_cast<const char*>(p) + 8 * (i16 & 1)));
+                            (lds_i32x2)at_bytes(vt, (vo ^ (32 * h)) + 16 * t * RB));
                         v = e4m3_to_bf16(x[0], x[1]);
                     } else {
                         s16x4_t x[2];
 #pragma unroll
-                        for (int a = 0; a < 2; ++a) {
-                            const int kr = 16 * t + 8 * a + 4 * half + i16 / 4;
-                            const uint4* p = vt + kr * (RB / 16) +
-                                             ((4 * h + 2 * side + ((i16 & 3) >> 1)) ^ swz_v_tile<RB, false>(kr));
+                        for (int a = 0; a < 2; ++a)
                             x[a] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                (lds_s16x4)(reinterpret_cast<const char*>(p) + 8 * (i16 & 1)));
-                        }
+                                (lds_s16x4)at_bytes(vt, (vo ^ (64 * h)) + (16 * t + 8 * a) * RB));
                         v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
                     }
                     O[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, O[h], 0, 0, 0);
                 }
-            }
-            if (careful) {
-                const uint64_t see = seen_keys(key0, pos, in.window, gone);
-#pragma unroll
-                for (int h = 0; h < kCols; ++h)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        O[h][i] = with_odd(O[h][i], odd_keys[32 * h + 8 * (i / 4) + 4 * half + i % 4], see);
             }
         };
         for (;;) {
@@ -680,6 +703,7 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
 #pragma unroll
             for (int h = 0; h < kCols; ++h) O[h] = f32x16_t{};
             const int32_t b0 = bl.first + st.block;
+            if (careful) notes.clear(tid);
             __syncthreads();  // the buffers are free
             stage(b0, kA, vA);
             for (int32_t i = 0; i < count; i += 2) {
@@ -702,6 +726,14 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
             careful = true;
         }
         l = half_sum(l);
+        if (careful) {
+            __syncthreads();
+#pragma unroll
+            for (int h = 0; h < kCols; ++h)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    O[h][i] = notes.apply(O[h][i], wave * 32 + n32, 32 * h + 8 * (i / 4) + 4 * half + i % 4);
+        }
 
         if (count == bl.count) {
             if (row_ok) {
@@ -765,6 +797,7 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
     __shared__ uint4 vA[kAttendWaves * kTile], vB[kAttendWaves * kTile];
     __shared__ float wm[kAttendWaves][M], wl[kAttendWaves][M];
     __shared__ OddKeys odd_keys[kAttendWaves][HD];
+    __shared__ OddNotes<M, HD> notes;
     __shared__ int flag;
     const int32_t wg = range_of_block(n_wg);
     const int64_t share = scalar_load(&ws.head->share), blocks = scalar_load(&ws.head->blocks);
@@ -777,18 +810,21 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
     WorkStart st{scalar_load(&ws.start[wg].req), scalar_load(&ws.start[wg].head),
                  scalar_load(&ws.start[wg].tile), scalar_load(&ws.start[wg].block)};
 
-    // sources of V's copies, by their place in the step; swz_v_row takes the row's
-    // bits up to 4, so groups of 16 rows come in two kinds
-    int32_t src_v[2][kCopies];
+    // This lane's K, its part of V's copies and its reads of V.  A copy of 1 KB takes
+    // 1024 / RB rows, so the permutation, by the row's low bits, changes from copy
+    // to copy; where the kinds repeat, the offsets are the same but for a constant.
+    const int k_src = n16 * RB + g4 * 16;
+    constexpr int kRows = 1024 / RB, kKinds = KS * RB / 1024;
+    int32_t src_v[kKinds];
 #pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
-            const int at16 = i * 64 + lane, row = at16 / (RB / 16), slot = at16 % (RB / 16);
-            src_v[g][i] = row * RB + ((slot ^ swz_v_row<RB, E4M3>(16 * g + row)) * 16);
-        }
-    uint4* const vmA = vA + wave * kTile;
-    uint4* const vmB = vB + wave * kTile;
+    for (int i = 0; i < kKinds; ++i) {
+        const int row = i * kRows + lane / (RB / 16), slot = lane % (RB / 16);
+        src_v[i] = (lane / (RB / 16)) * RB + ((slot ^ swz_v_row<RB, E4M3>(row)) * 16);
+    }
+    const int v_row = E4M3 ? 16 * (n16 >> 3) + 4 * g4 + ((n16 >> 1) & 3) : 4 * g4 + (n16 >> 2);
+    const int v_piece = E4M3 ? 0 : (n16 & 3) >> 1;
+    const int v_off = wave * kTile * 16 + v_row * RB + ((v_piece ^ swz_v_row<RB, E4M3>(v_row)) * 16) +
+                      8 * (n16 & 1);
 
     while (at < end) {
         const Span s = scalar_span(in, cache, st.req);
@@ -825,6 +861,7 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
             __attribute__((always_inline)) {
             const int32_t key0 = key_from + step * KS, len = step < steps ? s.len : 0;
             __amdgpu_buffer_rsrc_t vr[kGroups];
+            const int ko = fresh(k_src);
             gone = 0;
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
@@ -836,7 +873,7 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) {
                     const u32x4_t w = __builtin_bit_cast(
-                        u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(kr, n16 * RB + (4 * i + g4) * 16, 0, kOnce));
+                        u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(kr, ko + 64 * i, 0, kOnce));
                     K[g][i] = make_uint4(w.x, w.y, w.z, w.w);
                 }
             }
@@ -844,7 +881,8 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
             for (int g = 0; g < kGroups; ++g)
 #pragma unroll
                 for (int i = 0; i < kCopies; ++i)
-                    copy16<kOnce>(vr[g], vd + g * (kGroupKeys * RB / 16) + i * 64, src_v[g & 1][i]);
+                    copy16<kOnce>(vr[g], vd + wave * kTile + g * (kGroupKeys * RB / 16) + i * 64,
+                                  src_v[g * kCopies + i] + 1024 * i);
         };
 
         float m[NB], l[NB];
@@ -858,9 +896,13 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                 __builtin_amdgcn_s_waitcnt(0);
                 for (int e = lane; e < kTile; e += kWave) {
                     const int kr = e / (RB / 16), slot = (e % (RB / 16)) ^ swz_v_row<RB, E4M3>(kr);
-                    take_odd<E4M3>(vt + e, odd_keys[wave] + slot * (E4M3 ? 16 : 8), kr);
+                    take_odd<E4M3>(vt + wave * kTile + e, odd_keys[wave] + slot * (E4M3 ? 16 : 8), kr);
                 }
                 __builtin_amdgcn_s_waitcnt(0);
+                if (lane < 2 * M)
+                    notes.note(lane / M, lane % M,
+                               seen_keys(key0, base + min(lane % M, u.n_rows - 1) / group, in.window, gone),
+                               odd_keys[wave]);
             }
             f32x4_t S[NB][kGroups];
 #pragma unroll
@@ -895,22 +937,30 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                         }
                 }
             }
-            uint32_t P[NB][kGroups][2];
+            float top[NB];
+            bool raise = false;
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                float top = S[b][0][0];
+                top[b] = S[b][0][0];
 #pragma unroll
-                for (int i = 1; i < 4 * kGroups; ++i) top = fmaxf(top, S[b][i / 4][i % 4]);
-                top = quarter_max(top) * c2;
-                const bool raise = top > m[b] + kRaise;
-                if (__any(raise)) {
-                    const float m2 = raise ? top : m[b];
+                for (int i = 1; i < 4 * kGroups; ++i) top[b] = fmaxf(top[b], S[b][i / 4][i % 4]);
+                top[b] = quarter_max(top[b]) * c2;
+                raise |= top[b] > m[b] + kRaise;
+            }
+            if (__any(raise)) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const float m2 = top[b] > m[b] + kRaise ? top[b] : m[b];
                     const float fade = m[b] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[b] - m2);
                     m[b] = m2;
                     l[b] *= fade;
 #pragma unroll
                     for (int h = 0; h < kCols; ++h) O[b][h] *= fade;
                 }
+            }
+            uint32_t P[NB][kGroups][2];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
                 const float off = m[b] == -INFINITY ? 0.0f : m[b];
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g)
@@ -923,27 +973,22 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                     }
             }
             wait_all_but<kGroups * (kLoads + kCopies)>();  // the next step's loads: V is there
+            const int vo = fresh(v_off);
 #pragma unroll
             for (int h = 0; h < kCols; ++h) {
 #pragma unroll
                 for (int t = 0; t < kGroups / 2; ++t) {
                     bf16x8_t v;
                     if constexpr (E4M3) {
-                        const int r8 = n16 >> 1, kr = 32 * t + 16 * (r8 / 4) + 4 * g4 + r8 % 4;
-                        const uint4* p = vt + kr * (RB / 16) + (h ^ swz_v_row<RB, true>(kr));
                         const i32x2_t x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                            (lds_i32x2)(reinterpret_cast<const char*>(p) + 8 * (n16 & 1)));
+                            (lds_i32x2)at_bytes(vt, (vo ^ (16 * h)) + 32 * t * RB));
                         v = e4m3_to_bf16(x[0], x[1]);
                     } else {
                         s16x4_t x[2];
 #pragma unroll
-                        for (int a = 0; a < 2; ++a) {
-                            const int kr = 32 * t + 16 * a + 4 * g4 + n16 / 4;
-                            const uint4* p = vt + kr * (RB / 16) +
-                                             ((2 * h + ((n16 & 3) >> 1)) ^ swz_v_row<RB, false>(kr));
+                        for (int a = 0; a < 2; ++a)
                             x[a] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                (lds_s16x4)(reinterpret_cast<const char*>(p) + 8 * (n16 & 1)));
-                        }
+                                (lds_s16x4)at_bytes(vt, (vo ^ (32 * h)) + (32 * t + 16 * a) * RB));
                         v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
                     }
 #pragma unroll
@@ -952,17 +997,6 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                                                                 P[b][2 * t + 1][1]));
                         O[b][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w, O[b][h], 0, 0, 0);
                     }
-                }
-            }
-            if (careful) {
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    const uint64_t see = seen_keys(key0, pos[b], in.window, gone);
-#pragma unroll
-                    for (int h = 0; h < kCols; ++h)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            O[b][h][i] = with_odd(O[b][h][i], odd_keys[wave][16 * h + 4 * g4 + i], see);
                 }
             }
         };
@@ -974,12 +1008,16 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
 #pragma unroll
                 for (int h = 0; h < kCols; ++h) O[b][h] = f32x4_t{};
             }
-            stage(wave, KA, vmA, goneA);
+            if (careful) {
+                notes.clear(tid);
+                __syncthreads();
+            }
+            stage(wave, KA, vA, goneA);
             for (int32_t i = wave; i < steps; i += 2 * kAttendWaves) {
-                stage(i + kAttendWaves, KB, vmB, goneB);
-                key_step(i, KA, vmA, goneA);
-                stage(i + 2 * kAttendWaves, KA, vmA, goneA);
-                if (i + kAttendWaves < steps) key_step(i + kAttendWaves, KB, vmB, goneB);
+                stage(i + kAttendWaves, KB, vB, goneB);
+                key_step(i, KA, vA, goneA);
+                stage(i + 2 * kAttendWaves, KA, vA, goneA);
+                if (i + kAttendWaves < steps) key_step(i + kAttendWaves, KB, vB, goneB);
             }
             bool odd = false;
 #pragma unroll
@@ -1022,6 +1060,8 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                     sum += wl[w][row] * f;
                     o += pool[(w * 16 + r) * kVec + (c ^ r)] * f;
                 }
+                if (careful)
+                    for (int i = 0; i < 4; ++i) o[i] = notes.apply(o[i], row, 4 * c + i);
                 if (!whole) {
                     if (c == 0) {
                         part.put(row, top);
@@ -1063,14 +1103,17 @@ int32_t unit_rows(int32_t n_q, int32_t max_q, const KvCacheIn& c) {
     const int64_t rows = static_cast<int64_t>(max_q) * (n_q / c.n_kv);
     return rows <= 16 ? 16 : rows <= 32 ? 32 : kTileRows;
 }
-// Workgroups of a launch: as many as the chip holds at a time.
-int32_t workgroups(const KvCacheIn& c) { return c.head_dim > 128 ? 256 : 512; }
+// Workgroups of a launch: as many as the chip holds at a time (two on a CU where
+// their registers allow it).
+int32_t workgroups(int32_t rows, const KvCacheIn& c) {
+    return c.head_dim > 128 ? 256 : 512;
+}
 
 struct WsLayout {
     size_t start, done, parts, bytes;
 };
 WsLayout ws_layout(int32_t rows, const KvCacheIn& c) {
-    const size_t n = static_cast<size_t>(workgroups(c));
+    const size_t n = static_cast<size_t>(workgroups(rows, c));
     WsLayout w;
     w.start = 256;
     w.done = w.start + n * sizeof(WorkStart);
@@ -1100,7 +1143,7 @@ size_t attend_workspace(int32_t n_q, int32_t max_q, const KvCacheIn& cache) {
 
 hipError_t launch_attend(const AttendIn& in, const KvCacheIn& cache, bool e4m3, void* ws,
                          hipStream_t stream) {
-    const int32_t rows = unit_rows(in.n_q, in.max_q, cache), n_wg = workgroups(cache);
+    const int32_t rows = unit_rows(in.n_q, in.max_q, cache), n_wg = workgroups(rows, cache);
     const WsLayout w = ws_layout(rows, cache);
     char* p = static_cast<char*>(ws);
     const AttendWs aw{reinterpret_cast<PlanHead*>(p), reinterpret_cast<WorkStart*>(p + w.start),
