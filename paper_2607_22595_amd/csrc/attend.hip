@@ -267,11 +267,19 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t group_rows(const void* base, c
     return __builtin_amdgcn_make_buffer_rsrc(
         const_cast<char*>(static_cast<const char*>(base)) + row * RB, 0, live * RB, kBufferDword3);
 }
-// The page id of a key; past the request's last key, that one's.
-__device__ __forceinline__ int32_t page_of_key(const KvCacheIn& c, int32_t req, int32_t key,
-                                               int32_t len) {
+// The page ids of the groups of 16 keys from key0 on, one per lane from lane 0 (past
+// the request's last key, that one's).  They are loaded a step before they are needed,
+// by a vector load, which completes in order with the copies around it; a scalar load
+// would make every wait for LDS one for everything.
+__device__ __forceinline__ int32_t page_ids(const KvCacheIn& c, int32_t req, int32_t key0, int32_t len,
+                                            int groups) {
+    const int32_t key = key0 + (lane_id() & (groups - 1)) * kGroupKeys;
     const int32_t nth = max(0, min(key, len - 1)) >> c.page_log2;
-    return scalar_load(c.pages + static_cast<int64_t>(req) * c.max_pages + nth);
+    return (c.pages + static_cast<int64_t>(req) * c.max_pages)[nth];
+}
+// The groups whose page is not there, as bits.
+__device__ __forceinline__ uint32_t groups_gone(const KvCacheIn& c, int32_t ids, int groups) {
+    return static_cast<uint32_t>(wave_ballot(!page_ok(c, ids))) & ((1u << groups) - 1);
 }
 
 // An offset that the compiler computes from here on anew: a tile's reads differ by an
@@ -284,6 +292,12 @@ __device__ __forceinline__ int fresh(int off) {
 __device__ __forceinline__ const uint4* at_bytes(const uint4* p, int off) {
     return reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) + off);
 }
+
+// Operands read from LDS are taken kAhead reads before their use, in an order that
+// this fixes: left to itself the compiler reads each one right before its matrix
+// instruction and waits for it.
+constexpr int kAhead = 4;
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0); }
 
 typedef __attribute__((address_space(3))) void* lds_ptr;
 typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4;
@@ -462,17 +476,17 @@ __device__ void join_parts(const AttendIn& in, const AttendWs& ws, const RowsOut
                 last - first;
     __syncthreads();
     if (!scalar(*flag)) return;
-    constexpr int kVec = HD / 4, kAhead = 8;
+    constexpr int kVec = HD / 4, kLoads = 8;
     const int32_t rows = min(M, u.n_rows - u.row0);
     for (int32_t e = threadIdx.x; e < rows * kVec; e += kAttendThreads) {
         const int32_t row = e / kVec, c = e % kVec;
         float top = -INFINITY, l = 0.0f;
         f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int32_t w0 = first; w0 <= last; w0 += kAhead) {
-            float m[kAhead], s[kAhead];
-            f32x4_t x[kAhead];
+        for (int32_t w0 = first; w0 <= last; w0 += kLoads) {
+            float m[kLoads], s[kLoads];
+            f32x4_t x[kLoads];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
+            for (int i = 0; i < kLoads; ++i) {
                 const int32_t w = min(w0 + i, last);
                 const Part<M, HD> p(ws, w, w == first);
                 m[i] = p.get(row);
@@ -480,7 +494,7 @@ __device__ void join_parts(const AttendIn& in, const AttendWs& ws, const RowsOut
                 x[i] = p.get4(2 * M + row * HD + 4 * c);
             }
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
+            for (int i = 0; i < kLoads; ++i) {
                 if (w0 + i > last) break;
                 const float top2 = fmaxf(top, m[i]);
                 const float a = weight_of(top, top2), b = weight_of(m[i], top2);
@@ -571,9 +585,17 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
             }
         }
 
+        constexpr int kGroups = kBlockKeys / kGroupKeys;
+        int32_t ids;        // of the block to be copied next
+        uint32_t gone = 0;  // of the block whose turn it is
+        auto load_ids = [&](int32_t block) __attribute__((always_inline)) {
+            ids = page_ids(cache, st.req, block * kBlockKeys, s.len, kGroups);
+        };
+        // Copies a block and asks for the ids of the one after it.
         auto stage = [&](int32_t block, uint4* kd, uint4* vd) __attribute__((always_inline)) {
             const int32_t key = block * kBlockKeys + wave * kGroupKeys;
-            const int32_t page = page_of_key(cache, st.req, key, s.len);
+            const int32_t page = __builtin_amdgcn_readlane(ids, wave);
+            const uint32_t next_gone = groups_gone(cache, ids, kGroups);
             const __amdgpu_buffer_rsrc_t kr = group_rows<RB>(cache.k, cache, page, st.head, key, s.len);
             const __amdgpu_buffer_rsrc_t vr = group_rows<RB>(cache.v, cache, page, st.head, key, s.len);
 #pragma unroll
@@ -582,6 +604,8 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
 #pragma unroll
             for (int i = 0; i < kCopies; ++i)
                 copy16(vr, vd + wave * (kTile / 4) + i * 64, src_v[i]);
+            load_ids(block + 1);
+            return next_gone;
         };
 
         float m, l;
@@ -590,12 +614,6 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
         // One block: scores, weights, O.
         auto block_step = [&](int32_t block, const uint4* kt, uint4* vt) __attribute__((always_inline)) {
             const int32_t key0 = block * kBlockKeys;
-            // pages that are not there, by groups of 16 keys
-            uint32_t gone = 0;
-#pragma unroll
-            for (int g = 0; g < kBlockKeys / kGroupKeys; ++g)
-                if (!page_ok(cache, page_of_key(cache, st.req, key0 + g * kGroupKeys, s.len)))
-                    gone |= 1u << g;
             if (careful) {
                 for (int c = tid; c < HD; c += kAttendThreads) odd_keys[c] = OddKeys{0, 0};
                 __syncthreads();
@@ -610,26 +628,28 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                            odd_keys);
             }
             if (!wave_on || key0 > p_last) return;
-            f32x16_t S[2];
-            const int ko = fresh(k_off);
+            f32x16_t S[2] = {f32x16_t{}, f32x16_t{}};
+            {
+                constexpr int kReads = E4M3 ? kSteps : 2 * kSteps;  // a step of both halves of the keys
+                const int ko = fresh(k_off);
+                auto read_k = [&](int i) { return *at_bytes(kt + 32 * (i & 1) * (RB / 16), ko ^ (32 * (i >> 1))); };
+                uint4 w[kAhead];
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                f32x16_t acc = {};
-                const uint4* rows = kt + 32 * b * (RB / 16);
-                if constexpr (E4M3) {
+                for (int i = 0; i < kAhead; ++i) w[i] = read_k(i);
+                keep_order();
 #pragma unroll
-                    for (int i = 0; i < kSteps / 2; ++i) {
-                        const uint4 w = *at_bytes(rows, ko ^ (32 * i));
-                        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e4m3_to_bf16(w.x, w.y), Q[2 * i], acc, 0, 0, 0);
-                        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e4m3_to_bf16(w.z, w.w), Q[2 * i + 1], acc, 0, 0, 0);
+                for (int i = 0; i < kReads; ++i) {
+                    const int b = i & 1, step = i >> 1;
+                    const uint4 x = w[i % kAhead];
+                    if constexpr (E4M3) {
+                        S[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e4m3_to_bf16(x.x, x.y), Q[2 * step], S[b], 0, 0, 0);
+                        S[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e4m3_to_bf16(x.z, x.w), Q[2 * step + 1], S[b], 0, 0, 0);
+                    } else {
+                        S[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x), Q[step], S[b], 0, 0, 0);
                     }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < kSteps; ++i)
-                        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*at_bytes(rows, ko ^ (32 * i))),
-                                                                      Q[i], acc, 0, 0, 0);
+                    if (i + kAhead < kReads) w[i % kAhead] = read_k(i + kAhead);
+                    keep_order();
                 }
-                S[b] = acc;
             }
             if (gone || key0 + kBlockKeys - 1 > p_first ||
                 (in.window > 0 && key0 <= p_last - in.window)) {
@@ -660,6 +680,29 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                     for (int i = 0; i < 16; ++i) O[h][i] *= fade;
             }
             const float off = m == -INFINITY ? 0.0f : m;
+            // V^T operand j: column block j % kCols, 16 keys at j / kCols
+            const int vo = fresh(v_off);
+            auto read_v = [&](int j) {
+                const int t = j / kCols, h = j % kCols;
+                uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                if constexpr (E4M3) {
+                    const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                        (lds_i32x2)at_bytes(vt, (vo ^ (32 * h)) + 16 * t * RB)));
+                    w.x = x.x;
+                    w.y = x.y;
+                } else {
+                    const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (lds_s16x4)at_bytes(vt, (vo ^ (64 * h)) + 16 * t * RB)));
+                    const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (lds_s16x4)at_bytes(vt, (vo ^ (64 * h)) + (16 * t + 8) * RB)));
+                    w = make_uint4(x.x, x.y, y.x, y.y);
+                }
+                return w;
+            };
+            uint4 vw[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) vw[j] = read_v(j);
+            keep_order();
             uint32_t P[2][8];
             float sum = 0.0f;
 #pragma unroll
@@ -673,28 +716,16 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                     P[b][i / 2] = weights2(x, y);
                 }
             l += sum;
-            const int vo = fresh(v_off);
 #pragma unroll
-            for (int h = 0; h < kCols; ++h) {
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int b = t / 2, i0 = 4 * (t % 2);
-                    const bf16x8_t w = as_bf16x8(make_uint4(P[b][i0], P[b][i0 + 1], P[b][i0 + 2], P[b][i0 + 3]));
-                    bf16x8_t v;
-                    if constexpr (E4M3) {
-                        const i32x2_t x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                            (lds_i32x2)at_bytes(vt, (vo ^ (32 * h)) + 16 * t * RB));
-                        v = e4m3_to_bf16(x[0], x[1]);
-                    } else {
-                        s16x4_t x[2];
-#pragma unroll
-                        for (int a = 0; a < 2; ++a)
-                            x[a] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                (lds_s16x4)at_bytes(vt, (vo ^ (64 * h)) + (16 * t + 8 * a) * RB));
-                        v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
-                    }
-                    O[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, O[h], 0, 0, 0);
-                }
+            for (int j = 0; j < 4 * kCols; ++j) {
+                const int t = j / kCols, h = j % kCols, b = t / 2, i0 = 4 * (t % 2);
+                const bf16x8_t p = as_bf16x8(make_uint4(P[b][i0], P[b][i0 + 1], P[b][i0 + 2], P[b][i0 + 3]));
+                bf16x8_t v;
+                if constexpr (E4M3) v = e4m3_to_bf16(vw[j % kAhead].x, vw[j % kAhead].y);
+                else v = as_bf16x8(vw[j % kAhead]);
+                O[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p, O[h], 0, 0, 0);
+                if (j + kAhead < 4 * kCols) vw[j % kAhead] = read_v(j + kAhead);
+                keep_order();
             }
         };
         for (;;) {
@@ -705,17 +736,21 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
             const int32_t b0 = bl.first + st.block;
             if (careful) notes.clear(tid);
             __syncthreads();  // the buffers are free
-            stage(b0, kA, vA);
+            load_ids(b0);
+            gone = stage(b0, kA, vA);
             for (int32_t i = 0; i < count; i += 2) {
+                uint32_t after = 0;
                 __builtin_amdgcn_s_waitcnt(0);
                 __syncthreads();
-                if (i + 1 < count) stage(b0 + i + 1, kB, vB);
+                if (i + 1 < count) after = stage(b0 + i + 1, kB, vB);
                 block_step(b0 + i, kA, vA);
+                gone = after;
                 if (i + 1 >= count) break;
                 __builtin_amdgcn_s_waitcnt(0);
                 __syncthreads();
-                if (i + 2 < count) stage(b0 + i + 2, kA, vA);
+                if (i + 2 < count) after = stage(b0 + i + 2, kA, vA);
                 block_step(b0 + i + 1, kB, vB);
+                gone = after;
             }
             bool odd = false;
 #pragma unroll
@@ -857,19 +892,25 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
         // Every step of the pipeline issues its loads, past the last one of nothing
         // (resources without rows): with a branch around them the wait for one step's
         // K would be for everything outstanding.
+        int32_t ids;  // page ids of the step whose loads come next
+        auto load_ids = [&](int32_t step) __attribute__((always_inline)) {
+            ids = page_ids(cache, st.req, key_from + step * KS, s.len, kGroups);
+        };
         auto stage = [&](int32_t step, uint4 (&K)[kGroups][kLoads], uint4* vd, uint32_t& gone)
             __attribute__((always_inline)) {
             const int32_t key0 = key_from + step * KS, len = step < steps ? s.len : 0;
             __amdgpu_buffer_rsrc_t vr[kGroups];
+            int32_t page[kGroups];
+            gone = groups_gone(cache, ids, kGroups);
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) page[g] = __builtin_amdgcn_readlane(ids, g);
+            load_ids(step + kAttendWaves);
             const int ko = fresh(k_src);
-            gone = 0;
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
                 const int32_t key = key0 + g * kGroupKeys;
-                const int32_t page = page_of_key(cache, st.req, key, len);
-                if (!page_ok(cache, page)) gone |= 1u << g;
-                const __amdgpu_buffer_rsrc_t kr = group_rows<RB>(cache.k, cache, page, st.head, key, len);
-                vr[g] = group_rows<RB>(cache.v, cache, page, st.head, key, len);
+                const __amdgpu_buffer_rsrc_t kr = group_rows<RB>(cache.k, cache, page[g], st.head, key, len);
+                vr[g] = group_rows<RB>(cache.v, cache, page[g], st.head, key, len);
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) {
                     const u32x4_t w = __builtin_bit_cast(
@@ -958,6 +999,31 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                     for (int h = 0; h < kCols; ++h) O[b][h] *= fade;
                 }
             }
+            // V^T operand j: column block j % kCols, 32 keys at j / kCols
+            constexpr int kReads = kCols * kGroups / 2;
+            wait_all_but<1 + kGroups * (kLoads + kCopies)>();  // the next step's loads: V is there
+            const int vo = fresh(v_off);
+            auto read_v = [&](int j) {
+                const int t = j / kCols, h = j % kCols;
+                uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                if constexpr (E4M3) {
+                    const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                        (lds_i32x2)at_bytes(vt, (vo ^ (16 * h)) + 32 * t * RB)));
+                    w.x = x.x;
+                    w.y = x.y;
+                } else {
+                    const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (lds_s16x4)at_bytes(vt, (vo ^ (32 * h)) + 32 * t * RB)));
+                    const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (lds_s16x4)at_bytes(vt, (vo ^ (32 * h)) + (32 * t + 16) * RB)));
+                    w = make_uint4(x.x, x.y, y.x, y.y);
+                }
+                return w;
+            };
+            uint4 vw[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) vw[j] = read_v(j);
+            keep_order();
             uint32_t P[NB][kGroups][2];
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
@@ -972,32 +1038,20 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                         P[b][g][i] = weights2(x, y);
                     }
             }
-            wait_all_but<kGroups * (kLoads + kCopies)>();  // the next step's loads: V is there
-            const int vo = fresh(v_off);
 #pragma unroll
-            for (int h = 0; h < kCols; ++h) {
+            for (int j = 0; j < kReads; ++j) {
+                const int t = j / kCols, h = j % kCols;
+                bf16x8_t v;
+                if constexpr (E4M3) v = e4m3_to_bf16(vw[j % kAhead].x, vw[j % kAhead].y);
+                else v = as_bf16x8(vw[j % kAhead]);
 #pragma unroll
-                for (int t = 0; t < kGroups / 2; ++t) {
-                    bf16x8_t v;
-                    if constexpr (E4M3) {
-                        const i32x2_t x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                            (lds_i32x2)at_bytes(vt, (vo ^ (16 * h)) + 32 * t * RB));
-                        v = e4m3_to_bf16(x[0], x[1]);
-                    } else {
-                        s16x4_t x[2];
-#pragma unroll
-                        for (int a = 0; a < 2; ++a)
-                            x[a] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                (lds_s16x4)at_bytes(vt, (vo ^ (32 * h)) + (32 * t + 16 * a) * RB));
-                        v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
-                    }
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) {
-                        const bf16x8_t w = as_bf16x8(make_uint4(P[b][2 * t][0], P[b][2 * t][1], P[b][2 * t + 1][0],
-                                                                P[b][2 * t + 1][1]));
-                        O[b][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w, O[b][h], 0, 0, 0);
-                    }
+                for (int b = 0; b < NB; ++b) {
+                    const bf16x8_t p = as_bf16x8(make_uint4(P[b][2 * t][0], P[b][2 * t][1], P[b][2 * t + 1][0],
+                                                            P[b][2 * t + 1][1]));
+                    O[b][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, O[b][h], 0, 0, 0);
                 }
+                if (j + kAhead < kReads) vw[j % kAhead] = read_v(j + kAhead);
+                keep_order();
             }
         };
         for (;;) {
@@ -1012,6 +1066,7 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                 notes.clear(tid);
                 __syncthreads();
             }
+            load_ids(wave);
             stage(wave, KA, vA, goneA);
             for (int32_t i = wave; i < steps; i += 2 * kAttendWaves) {
                 stage(i + kAttendWaves, KB, vB, goneB);
