@@ -53,6 +53,7 @@ constexpr int kGroupKeys = 16;     // keys that surely lie in one page
 constexpr int kTileRows = 128;     // rows of a unit of the tile kernel
 constexpr int kMaxRequests = 4096;
 constexpr int kPlanThreads = 1024;
+constexpr int kWholeUnit = 18;    // units of so many blocks are not cut (tile kernel)
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 // A running maximum is raised only by a score this far above it (powers of two): the
 // weights stay below 2^8, which neither fp32 sums nor bf16 weights mind, and the
@@ -60,15 +61,17 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 constexpr float kRaise = 8.0f;
 
 struct WorkStart {  // where a workgroup's range begins
+    int64_t at;     // the unit's place, counted in blocks over all units
     int32_t req, head, tile, block;
 };
-struct PlanHead {
-    int64_t blocks, share;  // of all units; of one workgroup
-};
-// The workspace: plan head, a start per workgroup, a count of finished parts per
-// workgroup that begins a cut unit, and two parts per workgroup.
+// What a unit costs beside its blocks (its queries, the first copies, its rows), in
+// blocks: ranges of units of one block each took three times as long as others.
+constexpr int kTileExtra = 3, kRowExtra = 4;
+// The workspace: the blocks of one range before its ends are moved, a start per
+// workgroup and the end of the last one, a count of finished parts per workgroup that
+// begins a cut unit, and two parts per workgroup.
 struct AttendWs {
-    PlanHead* head;
+    int64_t* share;
     WorkStart* start;
     int32_t* done;
     float* parts;
@@ -76,7 +79,7 @@ struct AttendWs {
 template <>
 struct ArgPointers<AttendWs> {
     static std::vector<uint16_t> offsets() {
-        return {offsetof(AttendWs, head), offsetof(AttendWs, start), offsetof(AttendWs, done),
+        return {offsetof(AttendWs, share), offsetof(AttendWs, start), offsetof(AttendWs, done),
                 offsetof(AttendWs, parts)};
     }
 };
@@ -147,10 +150,14 @@ __device__ __forceinline__ int64_t wave_sum64(int64_t v) {
 
 // One workgroup.  Blocks of each request (a thread each, or where a request has
 // many tiles a wave each), their prefix, then the start of every range by a search
-// in the prefix and a walk over the request's tiles.
+// in the prefix and a walk over the request's tiles.  A range that would begin inside
+// a short unit (up to `whole` blocks) begins at the nearer end of it
+// instead: in the tile kernel a cut unit costs its parts' way through memory, 64 KB
+// each, and sixteen prompts of 128 to 1024 tokens take 245 us with every end cut and
+// 195 so.
 __global__ void __launch_bounds__(kPlanThreads)
 attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int32_t n_wg,
-                   int32_t least, int32_t many) {
+                   int32_t least, int32_t whole, int32_t extra, int32_t many) {
     __shared__ int64_t upto[kMaxRequests + 1];
     __shared__ int64_t wave_total[kPlanThreads / kWave];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -161,7 +168,7 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
             const Span s = span_of(in, cache, r, &bad);
             const int32_t tiles = tiles_of(s.n, group, rows);
             int64_t sum = 0;
-            for (int32_t t = 0; t < tiles; ++t) sum += blocks_of(s, t, group, rows, in.window).count;
+            for (int32_t t = 0; t < tiles; ++t) sum += blocks_of(s, t, group, rows, in.window).count + extra;
             upto[r + 1] = sum * cache.n_kv;
         }
     } else {
@@ -170,7 +177,7 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
             const int32_t tiles = tiles_of(s.n, group, rows);
             int64_t sum = 0;
             for (int32_t t = lane; t < tiles; t += kWave)
-                sum += blocks_of(s, t, group, rows, in.window).count;
+                sum += blocks_of(s, t, group, rows, in.window).count + extra;
             sum = wave_sum64(sum);
             if (lane == 0) upto[r + 1] = sum * cache.n_kv;
         }
@@ -200,11 +207,9 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
     __syncthreads();
     const int64_t blocks = upto[R];
     const int64_t share = max(static_cast<int64_t>(least), (blocks + n_wg - 1) / n_wg);
-    if (tid == 0) *ws.head = PlanHead{blocks, share};
-    for (int32_t w = tid; w < n_wg; w += kPlanThreads) {
-        ws.done[w] = 0;
-        const int64_t at = w * share;
-        if (at >= blocks) continue;
+    if (tid == 0) *ws.share = share;
+    // the unit and its block at position `at`, and the unit's blocks
+    auto locate = [&](int64_t at, int32_t* count) {
         int32_t lo = 0, hi = R - 1;  // the last request that starts at or before `at`
         while (lo < hi) {
             const int32_t mid = (lo + hi + 1) >> 1;
@@ -213,15 +218,31 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
         }
         const Span s = span_of(in, cache, lo);
         const int64_t a_head = (upto[lo + 1] - upto[lo]) / cache.n_kv, rest = at - upto[lo];
-        WorkStart st{lo, static_cast<int32_t>(rest / a_head), 0, 0};
+        WorkStart st{at, lo, static_cast<int32_t>(rest / a_head), 0, 0};
         int64_t left = rest % a_head;
         for (;;) {
-            const int32_t count = blocks_of(s, st.tile, group, rows, in.window).count;
-            if (left < count) break;
-            left -= count;
+            *count = blocks_of(s, st.tile, group, rows, in.window).count;
+            if (left < *count + extra) break;
+            left -= *count + extra;
             ++st.tile;
         }
-        st.block = static_cast<int32_t>(left);
+        st.at -= left;  // the unit's own
+        st.block = static_cast<int32_t>(max(static_cast<int64_t>(0), left - extra));
+        return st;
+    };
+    for (int32_t w = tid; w <= n_wg; w += kPlanThreads) {
+        if (w < n_wg) ws.done[w] = 0;
+        WorkStart st{blocks, 0, 0, 0, 0};
+        int32_t count;
+        if (w * share < blocks) {
+            st = locate(w * share, &count);
+            if (count <= whole && st.block != 0) {
+                const bool next = 2 * st.block > count;
+                st.block = 0;
+                if (next) st.at += count + extra;
+                if (next && st.at < blocks) st = locate(st.at, &count);
+            }
+        }
         ws.start[w] = st;
     }
 }
@@ -464,19 +485,19 @@ __device__ __forceinline__ float weight_of(float m, float top) {
     return m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
 }
 
-// After this workgroup's part is written: the last of the unit's workgroups joins
-// the parts, in their order, and writes the rows.
+// After this workgroup's part has reached memory (a wait by every wave, and a
+// barrier): the last of the unit's workgroups joins the parts, in their order, and
+// writes the rows.
 template <int M, int HD>
 __device__ void join_parts(const AttendIn& in, const AttendWs& ws, const RowsOut& u, int32_t first,
                            int32_t last, float v_scale, int* flag) {
-    __builtin_amdgcn_s_waitcnt(0);  // this wave's stores have reached memory
-    __syncthreads();
     if (threadIdx.x == 0)
         *flag = __hip_atomic_fetch_add(ws.done + first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
                 last - first;
     __syncthreads();
     if (!scalar(*flag)) return;
-    constexpr int kVec = HD / 4, kLoads = 8;
+    // parts in flight at a time (units of many rows are cut into few)
+    constexpr int kVec = HD / 4, kLoads = M >= kTileRows ? 2 : 8;
     const int32_t rows = min(M, u.n_rows - u.row0);
     for (int32_t e = threadIdx.x; e < rows * kVec; e += kAttendThreads) {
         const int32_t row = e / kVec, c = e % kVec;
@@ -529,17 +550,22 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
     __shared__ uint4 kA[kTile], kB[kTile], vA[kTile], vB[kTile];
     __shared__ OddKeys odd_keys[HD];
     __shared__ OddNotes<kTileRows, HD> notes;
-    __shared__ int flag;
+    __shared__ int flag, odd_unit;  // the last of this workgroup's units with values that are not finite
     const int32_t wg = range_of_block(n_wg);
-    const int64_t share = scalar_load(&ws.head->share), blocks = scalar_load(&ws.head->blocks);
-    int64_t at = wg * share;
-    const int64_t end = min(at + share, blocks);
-    if (at >= end) return;
+    const WorkStart* const from = ws.start + wg;
+    const int64_t share = scalar_load(ws.share);
+    const int32_t end_block = scalar_load(&from[1].block);
+    const int64_t end = scalar_load(&from[1].at) + (end_block ? kTileExtra + end_block : 0);
+    int64_t at = scalar_load(&from->at);
+    WorkStart st{at, scalar_load(&from->req), scalar_load(&from->head), scalar_load(&from->tile),
+                 scalar_load(&from->block)};
+    if (at + (st.block ? kTileExtra + st.block : 0) >= end) return;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, n32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int32_t group = in.n_q / cache.n_kv;
-    WorkStart st{scalar_load(&ws.start[wg].req), scalar_load(&ws.start[wg].head),
-                 scalar_load(&ws.start[wg].tile), scalar_load(&ws.start[wg].block)};
+    int unit = 0;
+    if (tid == 0) odd_unit = -1;
+    __syncthreads();
 
     // this lane's sources within a group of 16 rows, and its reads of a block
     int32_t src_k[kCopies], src_v[kCopies];
@@ -560,10 +586,11 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
         const Span s = scalar_span(in, cache, st.req);
         const int32_t tiles = tiles_of(s.n, group, kTileRows);
         const Blocks bl = blocks_of(s, st.tile, group, kTileRows, in.window);
-        const int32_t count = static_cast<int32_t>(min(static_cast<int64_t>(bl.count - st.block), end - at));
+        const int32_t count =
+            static_cast<int32_t>(min(static_cast<int64_t>(bl.count - st.block), end - (at + kTileExtra + st.block)));
         const RowsOut u{s.lo, s.n * group, st.tile * kTileRows, st.head, group};
-        const float ks = E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f;
-        const float c2 = in.scale * ks * kLog2e;
+        const float c2 = in.scale * (E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f) * kLog2e;
+        const float v_scale = E4M3 ? scalar_load(cache.v_scale + st.head) : 1.0f;
         // this lane's row, and the tokens of the wave's rows
         const int32_t row = u.row0 + wave * 32 + n32;
         const bool row_ok = row < u.n_rows;
@@ -734,8 +761,10 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
 #pragma unroll
             for (int h = 0; h < kCols; ++h) O[h] = f32x16_t{};
             const int32_t b0 = bl.first + st.block;
-            if (careful) notes.clear(tid);
-            __syncthreads();  // the buffers are free
+            if (careful) {
+                notes.clear(tid);
+                __syncthreads();
+            }
             load_ids(b0);
             gone = stage(b0, kA, vA);
             for (int32_t i = 0; i < count; i += 2) {
@@ -752,57 +781,63 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                 block_step(b0 + i + 1, kB, vB);
                 gone = after;
             }
-            bool odd = false;
+            // any value of O that is not finite makes this NaN
+            float odd = 0.0f;
 #pragma unroll
             for (int h = 0; h < kCols; ++h)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) odd |= !(fabsf(O[h][i]) < INFINITY);
-            if (careful || !scalar(__syncthreads_or(odd))) break;
-            careful = true;
-        }
-        l = half_sum(l);
-        if (careful) {
-            __syncthreads();
+                for (int i = 0; i < 16; ++i) odd = __builtin_fmaf(O[h][i], 0.0f, odd);
+            if (__any(odd != odd) && lane == 0) odd_unit = unit;
+            l = half_sum(l);
+            if (careful) {
+                __syncthreads();
 #pragma unroll
-            for (int h = 0; h < kCols; ++h)
+                for (int h = 0; h < kCols; ++h)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    O[h][i] = notes.apply(O[h][i], wave * 32 + n32, 32 * h + 8 * (i / 4) + 4 * half + i % 4);
-        }
-
-        if (count == bl.count) {
-            if (row_ok) {
-                const float inv = l == 0.0f ? 0.0f : (E4M3 ? scalar_load(cache.v_scale + st.head) : 1.0f) / l;
-                uint16_t* out = out_row(in, u, wave * 32 + n32, HD);
+                    for (int i = 0; i < 16; ++i)
+                        O[h][i] = notes.apply(O[h][i], wave * 32 + n32, 32 * h + 8 * (i / 4) + 4 * half + i % 4);
+            }
+            if (count == bl.count) {
+                if (row_ok) {
+                    const float inv = l == 0.0f ? 0.0f : v_scale / l;
+                    uint16_t* out = out_row(in, u, wave * 32 + n32, HD);
+#pragma unroll
+                    for (int h = 0; h < kCols; ++h)
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4)
+                            *reinterpret_cast<uint2*>(out + 32 * h + 2 * i + 4 * half) =
+                                make_uint2(weights2(O[h][i] * inv, O[h][i + 1] * inv),
+                                           weights2(O[h][i + 2] * inv, O[h][i + 3] * inv));
+                    if (half == 0) store_lse(in, u, wave * 32 + n32, m, l);
+                }
+            } else {
+                const Part<kTileRows, HD> part(ws, wg, st.block == 0);
+                const int r = wave * 32 + n32;
+                if (half == 0) {
+                    part.put(r, m);
+                    part.put(kTileRows + r, l);
+                }
 #pragma unroll
                 for (int h = 0; h < kCols; ++h)
 #pragma unroll
                     for (int i = 0; i < 16; i += 4)
-                        *reinterpret_cast<uint2*>(out + 32 * h + 2 * i + 4 * half) =
-                            make_uint2(pack_bf16(O[h][i] * inv, O[h][i + 1] * inv),
-                                       pack_bf16(O[h][i + 2] * inv, O[h][i + 3] * inv));
-                if (half == 0) store_lse(in, u, wave * 32 + n32, m, l);
+                        part.put4(2 * kTileRows + r * HD + 32 * h + 2 * i + 4 * half,
+                                  f32x4_t{O[h][i], O[h][i + 1], O[h][i + 2], O[h][i + 3]});
+                __builtin_amdgcn_s_waitcnt(0);
             }
-        } else {
-            const Part<kTileRows, HD> part(ws, wg, st.block == 0);
-            const int r = wave * 32 + n32;
-            if (half == 0) {
-                part.put(r, m);
-                part.put(kTileRows + r, l);
-            }
-#pragma unroll
-            for (int h = 0; h < kCols; ++h)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4)
-                    part.put4(2 * kTileRows + r * HD + 32 * h + 2 * i + 4 * half,
-                              f32x4_t{O[h][i], O[h][i + 1], O[h][i + 2], O[h][i + 3]});
-            const int64_t begin = at - st.block;
-            join_parts<kTileRows, HD>(in, ws, u, static_cast<int32_t>(begin / share),
-                                      static_cast<int32_t>((begin + bl.count - 1) / share),
-                                      E4M3 ? scalar_load(cache.v_scale + st.head) : 1.0f, &flag);
+            __syncthreads();  // the buffers are free, a part has reached memory, odd_unit is known
+            if (careful || scalar(odd_unit) != unit) break;
+            careful = true;
         }
+        if (count != bl.count) {
+            const int64_t begin = at + kTileExtra;
+            join_parts<kTileRows, HD>(in, ws, u, static_cast<int32_t>(begin / share),
+                                      static_cast<int32_t>((begin + bl.count - 1) / share), v_scale, &flag);
+        }
+        ++unit;
 
-        at += count;
+        if (st.block + count < bl.count) break;
+        at += kTileExtra + bl.count;
         st.block = 0;
         if (++st.tile == tiles) {
             st.tile = 0;
@@ -833,17 +868,22 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
     __shared__ float wm[kAttendWaves][M], wl[kAttendWaves][M];
     __shared__ OddKeys odd_keys[kAttendWaves][HD];
     __shared__ OddNotes<M, HD> notes;
-    __shared__ int flag;
+    __shared__ int flag, odd_unit;  // the last of this workgroup's units with values that are not finite
     const int32_t wg = range_of_block(n_wg);
-    const int64_t share = scalar_load(&ws.head->share), blocks = scalar_load(&ws.head->blocks);
-    int64_t at = wg * share;
-    const int64_t end = min(at + share, blocks);
-    if (at >= end) return;
+    const WorkStart* const from = ws.start + wg;
+    const int64_t share = scalar_load(ws.share);
+    const int32_t end_block = scalar_load(&from[1].block);
+    const int64_t end = scalar_load(&from[1].at) + (end_block ? kRowExtra + end_block : 0);
+    int64_t at = scalar_load(&from->at);
+    WorkStart st{at, scalar_load(&from->req), scalar_load(&from->head), scalar_load(&from->tile),
+                 scalar_load(&from->block)};
+    if (at + (st.block ? kRowExtra + st.block : 0) >= end) return;
     const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, n16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int32_t group = in.n_q / cache.n_kv;
-    WorkStart st{scalar_load(&ws.start[wg].req), scalar_load(&ws.start[wg].head),
-                 scalar_load(&ws.start[wg].tile), scalar_load(&ws.start[wg].block)};
+    int unit = 0;
+    if (tid == 0) odd_unit = -1;
+    __syncthreads();
 
     // This lane's K, its part of V's copies and its reads of V.  A copy of 1 KB takes
     // 1024 / RB rows, so the permutation, by the row's low bits, changes from copy
@@ -864,7 +904,8 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
     while (at < end) {
         const Span s = scalar_span(in, cache, st.req);
         const Blocks bl = blocks_of(s, 0, group, M, in.window);
-        const int32_t count = static_cast<int32_t>(min(static_cast<int64_t>(bl.count - st.block), end - at));
+        const int32_t count =
+            static_cast<int32_t>(min(static_cast<int64_t>(bl.count - st.block), end - (at + kRowExtra + st.block)));
         const RowsOut u{s.lo, s.n * group, 0, st.head, group};
         const float c2 = in.scale * (E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f) * kLog2e;
         const int32_t base = s.len - s.n;
@@ -1074,16 +1115,20 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                 stage(i + 2 * kAttendWaves, KA, vA, goneA);
                 if (i + kAttendWaves < steps) key_step(i + kAttendWaves, KB, vB, goneB);
             }
-            bool odd = false;
+            float odd = 0.0f;
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int h = 0; h < kCols; ++h)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) odd |= !(fabsf(O[b][h][i]) < INFINITY);
-            if (careful || !scalar(__syncthreads_or(odd))) break;
+                    for (int i = 0; i < 4; ++i) odd = __builtin_fmaf(O[b][h][i], 0.0f, odd);
+            if (__any(odd != odd) && lane == 0) odd_unit = unit;
+            __builtin_amdgcn_s_waitcnt(0);  // also the copies of steps past the last
+            __syncthreads();
+            if (careful || scalar(odd_unit) != unit) break;
             careful = true;
         }
+        ++unit;
 
         // the waves' rows joined in LDS (where V was), 16 at a time
         const bool whole = count == bl.count;
@@ -1132,13 +1177,16 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
             }
         }
         if (!whole) {
-            const int64_t begin = at - st.block;
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+            const int64_t begin = at + kRowExtra;
             join_parts<M, HD>(in, ws, u, static_cast<int32_t>(begin / share),
                               static_cast<int32_t>((begin + bl.count - 1) / share), v_scale, &flag);
         }
         __syncthreads();  // before V is copied in again
 
-        at += count;
+        if (st.block + count < bl.count) break;
+        at += kRowExtra + bl.count;
         st.block = 0;
         if (++st.head == cache.n_kv) {
             st.head = 0;
@@ -1171,8 +1219,8 @@ WsLayout ws_layout(int32_t rows, const KvCacheIn& c) {
     const size_t n = static_cast<size_t>(workgroups(rows, c));
     WsLayout w;
     w.start = 256;
-    w.done = w.start + n * sizeof(WorkStart);
-    w.parts = w.done + n * sizeof(int32_t);
+    w.done = w.start + (n + 1) * sizeof(WorkStart);
+    w.parts = (w.done + n * sizeof(int32_t) + 255) / 256 * 256;
     w.bytes = w.parts + 2 * n * rows * static_cast<size_t>(c.head_dim + 2) * sizeof(float);
     return w;
 }
@@ -1201,11 +1249,12 @@ hipError_t launch_attend(const AttendIn& in, const KvCacheIn& cache, bool e4m3, 
     const int32_t rows = unit_rows(in.n_q, in.max_q, cache), n_wg = workgroups(rows, cache);
     const WsLayout w = ws_layout(rows, cache);
     char* p = static_cast<char*>(ws);
-    const AttendWs aw{reinterpret_cast<PlanHead*>(p), reinterpret_cast<WorkStart*>(p + w.start),
+    const AttendWs aw{reinterpret_cast<int64_t*>(p), reinterpret_cast<WorkStart*>(p + w.start),
                       reinterpret_cast<int32_t*>(p + w.done), reinterpret_cast<float*>(p + w.parts)};
     const int64_t most = (static_cast<int64_t>(in.max_q) * (in.n_q / cache.n_kv) + rows - 1) / rows;
     hipLaunchKernelGGL(attend_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, in, cache, aw, rows,
-                       n_wg, rows == kTileRows ? 4 : 4, most > 4 ? 1 : 0);
+                       n_wg, rows == kTileRows ? 1 : 4, rows == kTileRows ? kWholeUnit : 0,
+                       rows == kTileRows ? kTileExtra : kRowExtra, most > 4 ? 1 : 0);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel_for(cache.head_dim, e4m3, rows), dim3(n_wg), dim3(kAttendThreads), 0, stream,
