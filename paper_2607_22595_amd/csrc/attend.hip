@@ -51,7 +51,7 @@ constexpr int kAttendThreads = 256, kAttendWaves = 4;
 constexpr int kBlockKeys = 64;     // keys of a block
 constexpr int kGroupKeys = 16;     // keys that surely lie in one page
 constexpr int kTileRows = 128;     // rows of a unit of the tile kernel
-constexpr int kMaxRequests = 4096;
+constexpr int kMaxRequests = 4096, kMaxRanges = 512;
 constexpr int kPlanThreads = 1024;
 constexpr int kWholeUnit = 18;    // units of so many blocks are not cut (tile kernel)
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -60,27 +60,30 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 // rescaling of O, rare after the first blocks, is skipped by a wave vote.
 constexpr float kRaise = 8.0f;
 
-struct WorkStart {  // where a workgroup's range begins
-    int64_t at;     // the unit's place, counted in blocks over all units
-    int32_t req, head, tile, block;
+// A workgroup's range, for the workgroup of that index in the launch: places counted
+// in blocks over all units.
+struct WorkRange {
+    int64_t at;                      // place of the unit it begins in
+    int64_t end;                     // where it ends
+    int64_t share;                   // blocks of a range before its ends were moved
+    int32_t req, head, tile, block;  // the unit, and its block that is the first
+    int32_t lo, n, len;              // the request's span and keys
+    int32_t nth;                     // its place among the ranges
 };
 // What a unit costs beside its blocks (its queries, the first copies, its rows), in
 // blocks: ranges of units of one block each took three times as long as others.
 constexpr int kTileExtra = 3, kRowExtra = 4;
-// The workspace: the blocks of one range before its ends are moved, a start per
-// workgroup and the end of the last one, a count of finished parts per workgroup that
-// begins a cut unit, and two parts per workgroup.
+// The workspace: a range per workgroup, a count of finished parts per range that
+// begins a cut unit, and two parts per range.
 struct AttendWs {
-    int64_t* share;
-    WorkStart* start;
+    WorkRange* range;
     int32_t* done;
     float* parts;
 };
 template <>
 struct ArgPointers<AttendWs> {
     static std::vector<uint16_t> offsets() {
-        return {offsetof(AttendWs, share), offsetof(AttendWs, start), offsetof(AttendWs, done),
-                offsetof(AttendWs, parts)};
+        return {offsetof(AttendWs, range), offsetof(AttendWs, done), offsetof(AttendWs, parts)};
     }
 };
 
@@ -158,7 +161,7 @@ __device__ __forceinline__ int64_t wave_sum64(int64_t v) {
 __global__ void __launch_bounds__(kPlanThreads)
 attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int32_t n_wg,
                    int32_t least, int32_t whole, int32_t extra, int32_t many) {
-    __shared__ int64_t upto[kMaxRequests + 1];
+    __shared__ int64_t upto[kMaxRequests + 1], begins[kMaxRanges + 1];
     __shared__ int64_t wave_total[kPlanThreads / kWave];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int32_t R = cache.R_max, group = in.n_q / cache.n_kv;
@@ -207,7 +210,6 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
     __syncthreads();
     const int64_t blocks = upto[R];
     const int64_t share = max(static_cast<int64_t>(least), (blocks + n_wg - 1) / n_wg);
-    if (tid == 0) *ws.share = share;
     // the unit and its block at position `at`, and the unit's blocks
     auto locate = [&](int64_t at, int32_t* count) {
         int32_t lo = 0, hi = R - 1;  // the last request that starts at or before `at`
@@ -218,7 +220,7 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
         }
         const Span s = span_of(in, cache, lo);
         const int64_t a_head = (upto[lo + 1] - upto[lo]) / cache.n_kv, rest = at - upto[lo];
-        WorkStart st{at, lo, static_cast<int32_t>(rest / a_head), 0, 0};
+        WorkRange st{at, 0, share, lo, static_cast<int32_t>(rest / a_head), 0, 0, s.lo, s.n, s.len, 0};
         int64_t left = rest % a_head;
         for (;;) {
             *count = blocks_of(s, st.tile, group, rows, in.window).count;
@@ -230,9 +232,13 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
         st.block = static_cast<int32_t>(max(static_cast<int64_t>(0), left - extra));
         return st;
     };
-    for (int32_t w = tid; w <= n_wg; w += kPlanThreads) {
-        if (w < n_wg) ws.done[w] = 0;
-        WorkStart st{blocks, 0, 0, 0, 0};
+    // The workgroups are dealt over the XCDs in turn; neighbouring ranges, which read
+    // the same keys, go to one XCD and its L2, and few ranges still to all of them.
+    const int32_t used = static_cast<int32_t>(min(static_cast<int64_t>(n_wg), (blocks + share - 1) / share));
+    const int32_t each = (used + 7) / 8;
+    const int32_t w = tid;  // (a thread per range)
+    WorkRange st{blocks, 0, share, 0, 0, 0, 0, 0, 0, 0, 0};
+    if (w <= n_wg) {
         int32_t count;
         if (w * share < blocks) {
             st = locate(w * share, &count);
@@ -243,7 +249,16 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
                 if (next && st.at < blocks) st = locate(st.at, &count);
             }
         }
-        ws.start[w] = st;
+        begins[w] = st.at + (st.block ? extra + st.block : 0);
+    }
+    __syncthreads();
+    if (w < n_wg) {
+        ws.done[w] = 0;
+        st.end = begins[w + 1];
+        if (begins[w] == st.end) st.end = st.at;  // nothing to do
+        st.nth = w;
+        // range w at each * (b % 8) + b / 8; the others behind them, in order
+        ws.range[w < 8 * each ? w / each + 8 * (w % each) : w] = st;
     }
 }
 
@@ -531,18 +546,19 @@ __device__ void join_parts(const AttendIn& in, const AttendWs& ws, const RowsOut
     }
 }
 
-// The workgroups are dealt over the XCDs in turn; neighbouring ranges, which read the
-// same keys, go to one XCD and its L2.
-__device__ __forceinline__ int32_t range_of_block(int32_t n_wg) {
-    const int32_t b = blockIdx.x;
-    return n_wg % 8 == 0 ? (b % 8) * (n_wg / 8) + b / 8 : b;
+// This workgroup's range.
+__device__ __forceinline__ WorkRange range_of(const AttendWs& ws) {
+    const WorkRange* r = ws.range + blockIdx.x;
+    return {scalar_load(&r->at), scalar_load(&r->end), scalar_load(&r->share), scalar_load(&r->req),
+            scalar_load(&r->head), scalar_load(&r->tile), scalar_load(&r->block), scalar_load(&r->lo),
+            scalar_load(&r->n), scalar_load(&r->len), scalar_load(&r->nth)};
 }
 
 // ---------------------------------------------------------------- tile kernel
 
 template <int HD, bool E4M3>
 __global__ void __launch_bounds__(kAttendThreads, HD > 128 ? 1 : 2)
-attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
+attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
     constexpr int RB = HD * (E4M3 ? 1 : 2);      // bytes of a cached row
     constexpr int kTile = kBlockKeys * RB / 16;  // pieces of a block
     constexpr int kCopies = kGroupKeys * RB / 1024;
@@ -551,15 +567,8 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
     __shared__ OddKeys odd_keys[HD];
     __shared__ OddNotes<kTileRows, HD> notes;
     __shared__ int flag, odd_unit;  // the last of this workgroup's units with values that are not finite
-    const int32_t wg = range_of_block(n_wg);
-    const WorkStart* const from = ws.start + wg;
-    const int64_t share = scalar_load(ws.share);
-    const int32_t end_block = scalar_load(&from[1].block);
-    const int64_t end = scalar_load(&from[1].at) + (end_block ? kTileExtra + end_block : 0);
-    int64_t at = scalar_load(&from->at);
-    WorkStart st{at, scalar_load(&from->req), scalar_load(&from->head), scalar_load(&from->tile),
-                 scalar_load(&from->block)};
-    if (at + (st.block ? kTileExtra + st.block : 0) >= end) return;
+    WorkRange st = range_of(ws);
+    if (st.at >= st.end) return;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, n32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int32_t group = in.n_q / cache.n_kv;
@@ -582,12 +591,11 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
     const int v_piece = E4M3 ? side : 2 * side + ((i16 & 3) >> 1);
     const int v_off = v_row * RB + ((v_piece ^ swz_v_tile<RB, E4M3>(v_row)) * 16) + 8 * (i16 & 1);
 
-    while (at < end) {
-        const Span s = scalar_span(in, cache, st.req);
+    for (Span s{st.lo, st.n, st.len}; st.at < st.end; s = scalar_span(in, cache, st.req)) {
         const int32_t tiles = tiles_of(s.n, group, kTileRows);
         const Blocks bl = blocks_of(s, st.tile, group, kTileRows, in.window);
         const int32_t count =
-            static_cast<int32_t>(min(static_cast<int64_t>(bl.count - st.block), end - (at + kTileExtra + st.block)));
+            static_cast<int32_t>(min(static_cast<int64_t>(bl.count - st.block), st.end - (st.at + kTileExtra + st.block)));
         const RowsOut u{s.lo, s.n * group, st.tile * kTileRows, st.head, group};
         const float c2 = in.scale * (E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f) * kLog2e;
         const float v_scale = E4M3 ? scalar_load(cache.v_scale + st.head) : 1.0f;
@@ -811,7 +819,7 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
                     if (half == 0) store_lse(in, u, wave * 32 + n32, m, l);
                 }
             } else {
-                const Part<kTileRows, HD> part(ws, wg, st.block == 0);
+                const Part<kTileRows, HD> part(ws, st.nth, st.block == 0);
                 const int r = wave * 32 + n32;
                 if (half == 0) {
                     part.put(r, m);
@@ -830,20 +838,20 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
             careful = true;
         }
         if (count != bl.count) {
-            const int64_t begin = at + kTileExtra;
-            join_parts<kTileRows, HD>(in, ws, u, static_cast<int32_t>(begin / share),
-                                      static_cast<int32_t>((begin + bl.count - 1) / share), v_scale, &flag);
+            const int64_t begin = st.at + kTileExtra;
+            join_parts<kTileRows, HD>(in, ws, u, static_cast<int32_t>(begin / st.share),
+                                      static_cast<int32_t>((begin + bl.count - 1) / st.share), v_scale, &flag);
         }
         ++unit;
 
         if (st.block + count < bl.count) break;
-        at += kTileExtra + bl.count;
+        st.at += kTileExtra + bl.count;
         st.block = 0;
         if (++st.tile == tiles) {
             st.tile = 0;
             if (++st.head == cache.n_kv) {
                 st.head = 0;
-                if (at < end)
+                if (st.at < st.end)
                     do ++st.req;
                     while (scalar_span(in, cache, st.req).n == 0);
             }
@@ -855,7 +863,7 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
 
 template <int HD, bool E4M3, int NB>
 __global__ void __launch_bounds__(kAttendThreads, HD > 128 ? 1 : 2)
-attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
+attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
     constexpr int RB = HD * (E4M3 ? 1 : 2);
     constexpr int KS = !E4M3 && RB >= 256 ? 32 : 64;  // keys of a step: 8 KB of V, or more
     constexpr int kGroups = KS / kGroupKeys;
@@ -869,15 +877,8 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
     __shared__ OddKeys odd_keys[kAttendWaves][HD];
     __shared__ OddNotes<M, HD> notes;
     __shared__ int flag, odd_unit;  // the last of this workgroup's units with values that are not finite
-    const int32_t wg = range_of_block(n_wg);
-    const WorkStart* const from = ws.start + wg;
-    const int64_t share = scalar_load(ws.share);
-    const int32_t end_block = scalar_load(&from[1].block);
-    const int64_t end = scalar_load(&from[1].at) + (end_block ? kRowExtra + end_block : 0);
-    int64_t at = scalar_load(&from->at);
-    WorkStart st{at, scalar_load(&from->req), scalar_load(&from->head), scalar_load(&from->tile),
-                 scalar_load(&from->block)};
-    if (at + (st.block ? kRowExtra + st.block : 0) >= end) return;
+    WorkRange st = range_of(ws);
+    if (st.at >= st.end) return;
     const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, n16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int32_t group = in.n_q / cache.n_kv;
@@ -901,11 +902,10 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
     const int v_off = wave * kTile * 16 + v_row * RB + ((v_piece ^ swz_v_row<RB, E4M3>(v_row)) * 16) +
                       8 * (n16 & 1);
 
-    while (at < end) {
-        const Span s = scalar_span(in, cache, st.req);
+    for (Span s{st.lo, st.n, st.len}; st.at < st.end; s = scalar_span(in, cache, st.req)) {
         const Blocks bl = blocks_of(s, 0, group, M, in.window);
         const int32_t count =
-            static_cast<int32_t>(min(static_cast<int64_t>(bl.count - st.block), end - (at + kRowExtra + st.block)));
+            static_cast<int32_t>(min(static_cast<int64_t>(bl.count - st.block), st.end - (st.at + kRowExtra + st.block)));
         const RowsOut u{s.lo, s.n * group, 0, st.head, group};
         const float c2 = in.scale * (E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f) * kLog2e;
         const int32_t base = s.len - s.n;
@@ -1133,7 +1133,7 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
         // the waves' rows joined in LDS (where V was), 16 at a time
         const bool whole = count == bl.count;
         const float v_scale = E4M3 ? scalar_load(cache.v_scale + st.head) : 1.0f;
-        const Part<M, HD> part(ws, wg, st.block == 0);
+        const Part<M, HD> part(ws, st.nth, st.block == 0);
         f32x4_t* const pool = reinterpret_cast<f32x4_t*>(vA);
         constexpr int kVec = HD / 4;
 #pragma unroll
@@ -1179,18 +1179,18 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t n_wg) {
         if (!whole) {
             __builtin_amdgcn_s_waitcnt(0);
             __syncthreads();
-            const int64_t begin = at + kRowExtra;
-            join_parts<M, HD>(in, ws, u, static_cast<int32_t>(begin / share),
-                              static_cast<int32_t>((begin + bl.count - 1) / share), v_scale, &flag);
+            const int64_t begin = st.at + kRowExtra;
+            join_parts<M, HD>(in, ws, u, static_cast<int32_t>(begin / st.share),
+                              static_cast<int32_t>((begin + bl.count - 1) / st.share), v_scale, &flag);
         }
         __syncthreads();  // before V is copied in again
 
         if (st.block + count < bl.count) break;
-        at += kRowExtra + bl.count;
+        st.at += kRowExtra + bl.count;
         st.block = 0;
         if (++st.head == cache.n_kv) {
             st.head = 0;
-            if (at < end)
+            if (st.at < st.end)
                 do ++st.req;
                 while (scalar_span(in, cache, st.req).n == 0);
         }
@@ -1213,19 +1213,18 @@ int32_t workgroups(int32_t rows, const KvCacheIn& c) {
 }
 
 struct WsLayout {
-    size_t start, done, parts, bytes;
+    size_t done, parts, bytes;
 };
 WsLayout ws_layout(int32_t rows, const KvCacheIn& c) {
     const size_t n = static_cast<size_t>(workgroups(rows, c));
     WsLayout w;
-    w.start = 256;
-    w.done = w.start + (n + 1) * sizeof(WorkStart);
-    w.parts = (w.done + n * sizeof(int32_t) + 255) / 256 * 256;
+    w.done = n * sizeof(WorkRange);
+    w.parts = w.done + n * sizeof(int32_t);
     w.bytes = w.parts + 2 * n * rows * static_cast<size_t>(c.head_dim + 2) * sizeof(float);
     return w;
 }
 
-using AttendKernel = void (*)(AttendIn, KvCacheIn, AttendWs, int32_t);
+using AttendKernel = void (*)(AttendIn, KvCacheIn, AttendWs);
 // Indexed by head_dim (64, 128, 256), type and form (16 rows, 32 rows, tiles).
 constexpr AttendKernel kKernels[3][2][3] = {
     {{attend_row_kernel<64, false, 1>, attend_row_kernel<64, false, 2>, attend_tile_kernel<64, false>},
@@ -1249,8 +1248,8 @@ hipError_t launch_attend(const AttendIn& in, const KvCacheIn& cache, bool e4m3, 
     const int32_t rows = unit_rows(in.n_q, in.max_q, cache), n_wg = workgroups(rows, cache);
     const WsLayout w = ws_layout(rows, cache);
     char* p = static_cast<char*>(ws);
-    const AttendWs aw{reinterpret_cast<int64_t*>(p), reinterpret_cast<WorkStart*>(p + w.start),
-                      reinterpret_cast<int32_t*>(p + w.done), reinterpret_cast<float*>(p + w.parts)};
+    const AttendWs aw{reinterpret_cast<WorkRange*>(p), reinterpret_cast<int32_t*>(p + w.done),
+                      reinterpret_cast<float*>(p + w.parts)};
     const int64_t most = (static_cast<int64_t>(in.max_q) * (in.n_q / cache.n_kv) + rows - 1) / rows;
     hipLaunchKernelGGL(attend_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, in, cache, aw, rows,
                        n_wg, rows == kTileRows ? 1 : 4, rows == kTileRows ? kWholeUnit : 0,
@@ -1258,7 +1257,7 @@ hipError_t launch_attend(const AttendIn& in, const KvCacheIn& cache, bool e4m3, 
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel_for(cache.head_dim, e4m3, rows), dim3(n_wg), dim3(kAttendThreads), 0, stream,
-                       in, cache, aw, n_wg);
+                       in, cache, aw);
     return hipGetLastError();
 }
 
