@@ -716,6 +716,11 @@ xmix_status xmix_paged_attention(const uint16_t* q, int64_t q_stride, int32_t n_
     in.window = window;
     in.max_q = max_q;
     in.scale = scale;
+    const int64_t n = n_q / c.n_kv;
+    in.group.n = static_cast<int32_t>(n);
+    in.group.mul = n > 1 && (max_q * n + 4096) * n < (int64_t{1} << 32)
+                       ? static_cast<uint32_t>((int64_t{1} << 32) / n + 1)
+                       : 0;
     return launched(launch_attend(in, c, cache->dt == XMIX_E4M3, ws, as_stream(stream)));
 }
 

@@ -126,17 +126,17 @@ __device__ __forceinline__ Span scalar_span(const AttendIn& in, const KvCacheIn&
 // A uniform value in a scalar register, where the compiler has put it in a vector one
 // (a resource made of it would be rebuilt lane by lane).
 __device__ __forceinline__ int32_t scalar(int32_t v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ int32_t tiles_of(int32_t n, int32_t group, int32_t rows) {
-    return static_cast<int32_t>((static_cast<int64_t>(n) * group + rows - 1) / rows);
+__device__ __forceinline__ int32_t tiles_of(int32_t n, const HeadGroup& group, int32_t rows) {
+    return static_cast<int32_t>((static_cast<uint32_t>(n) * group.n + rows - 1) / rows);
 }
 // The keys that some row of tile t sees, in blocks: [first, first + count), one block
 // at least (a tile without a key still has rows to write).
 struct Blocks {
     int32_t first, count;
 };
-__device__ __forceinline__ Blocks blocks_of(const Span& s, int32_t t, int32_t group, int32_t rows,
+__device__ __forceinline__ Blocks blocks_of(const Span& s, int32_t t, const HeadGroup& group, int32_t rows,
                                             int32_t window) {
-    const int32_t tok0 = t * rows / group, tok1 = min(((t + 1) * rows - 1) / group, s.n - 1);
+    const int32_t tok0 = group.div(t * rows), tok1 = min(group.div((t + 1) * rows - 1), s.n - 1);
     const int32_t hi = s.len - s.n + tok1 + 1, p0 = s.len - s.n + tok0;
     const int32_t lo = window > 0 && p0 >= window ? p0 - window + 1 : 0;
     const int32_t first = hi > 0 ? lo / kBlockKeys : 0;
@@ -164,7 +164,8 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
     __shared__ int64_t upto[kMaxRequests + 1], begins[kMaxRanges + 1];
     __shared__ int64_t wave_total[kPlanThreads / kWave];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int32_t R = cache.R_max, group = in.n_q / cache.n_kv;
+    const int32_t R = cache.R_max;
+    const HeadGroup group = in.group;
     bool bad = false;
     if (!many) {
         for (int32_t r = tid; r < R; r += kPlanThreads) {
@@ -482,37 +483,30 @@ struct Part {
 
 // The rows of a unit in the caller's tensors.
 struct RowsOut {
-    int32_t lo, n_rows, row0, head, group;  // first token of the span; its rows; the tile's first
+    int32_t lo, n_rows, row0, head;  // first token of the span; its rows; the tile's first
+    HeadGroup group;
 };
 __device__ __forceinline__ uint16_t* out_row(const AttendIn& in, const RowsOut& u, int32_t row,
                                              int hd) {
-    const int32_t at = u.row0 + row, tok = at / u.group, g = at - tok * u.group;
-    return in.out + (u.lo + tok) * in.out_stride + static_cast<int64_t>(u.head * u.group + g) * hd;
+    const int32_t at = u.row0 + row, tok = u.group.div(at), g = at - tok * u.group.n;
+    return in.out + (u.lo + tok) * in.out_stride + static_cast<int64_t>(u.head * u.group.n + g) * hd;
 }
 __device__ __forceinline__ void store_lse(const AttendIn& in, const RowsOut& u, int32_t row, float m,
                                           float l) {
     if (!in.lse) return;
-    const int32_t at = u.row0 + row, tok = at / u.group, g = at - tok * u.group;
-    in.lse[static_cast<int64_t>(u.head * u.group + g) * in.T_max + u.lo + tok] =
+    const int32_t at = u.row0 + row, tok = u.group.div(at), g = at - tok * u.group.n;
+    in.lse[static_cast<int64_t>(u.head * u.group.n + g) * in.T_max + u.lo + tok] =
         l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 __device__ __forceinline__ float weight_of(float m, float top) {
     return m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
 }
 
-// After this workgroup's part has reached memory (a wait by every wave, and a
-// barrier): the last of the unit's workgroups joins the parts, in their order, and
-// writes the rows.
-template <int M, int HD>
-__device__ void join_parts(const AttendIn& in, const AttendWs& ws, const RowsOut& u, int32_t first,
-                           int32_t last, float v_scale, int* flag) {
-    if (threadIdx.x == 0)
-        *flag = __hip_atomic_fetch_add(ws.done + first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
-                last - first;
-    __syncthreads();
-    if (!scalar(*flag)) return;
-    // parts in flight at a time (units of many rows are cut into few)
-    constexpr int kVec = HD / 4, kLoads = M >= kTileRows ? 2 : 8;
+// Joins the parts of a unit, kLoads of them in flight at a time.
+template <int M, int HD, int kLoads>
+__device__ __forceinline__ void join_rows(const AttendIn& in, const AttendWs& ws, const RowsOut& u,
+                                          int32_t first, int32_t last, float v_scale) {
+    constexpr int kVec = HD / 4;
     const int32_t rows = min(M, u.n_rows - u.row0);
     for (int32_t e = threadIdx.x; e < rows * kVec; e += kAttendThreads) {
         const int32_t row = e / kVec, c = e % kVec;
@@ -531,7 +525,11 @@ __device__ void join_parts(const AttendIn& in, const AttendWs& ws, const RowsOut
             }
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                if (w0 + i > last) break;
+                if (w0 + i > last) {  // (the last one again)
+                    m[i] = -INFINITY;
+                    s[i] = 0.0f;
+                    x[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+                }
                 const float top2 = fmaxf(top, m[i]);
                 const float a = weight_of(top, top2), b = weight_of(m[i], top2);
                 l = l * a + s[i] * b;
@@ -541,9 +539,23 @@ __device__ void join_parts(const AttendIn& in, const AttendWs& ws, const RowsOut
         }
         const float inv = l == 0.0f ? 0.0f : v_scale / l;
         *reinterpret_cast<uint2*>(out_row(in, u, row, HD) + 4 * c) =
-            make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+            make_uint2(weights2(o[0] * inv, o[1] * inv), weights2(o[2] * inv, o[3] * inv));
         if (c == 0) store_lse(in, u, row, top, l);
     }
+}
+// After this workgroup's part has reached memory (a wait by every wave, and a
+// barrier): the last of the unit's workgroups joins the parts, in their order, and
+// writes the rows.
+template <int M, int HD>
+__device__ void join_parts(const AttendIn& in, const AttendWs& ws, const RowsOut& u, int32_t first,
+                           int32_t last, float v_scale, int* flag) {
+    if (threadIdx.x == 0)
+        *flag = __hip_atomic_fetch_add(ws.done + first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+                last - first;
+    __syncthreads();
+    if (!scalar(*flag)) return;
+    if (last - first < 4 || M >= kTileRows) join_rows<M, HD, 4>(in, ws, u, first, last, v_scale);
+    else join_rows<M, HD, 16>(in, ws, u, first, last, v_scale);
 }
 
 // This workgroup's range.
@@ -571,7 +583,7 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
     if (st.at >= st.end) return;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, n32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int32_t group = in.n_q / cache.n_kv;
+    const HeadGroup group = in.group;
     int unit = 0;
     if (tid == 0) odd_unit = -1;
     __syncthreads();
@@ -596,23 +608,23 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
         const Blocks bl = blocks_of(s, st.tile, group, kTileRows, in.window);
         const int32_t count =
             static_cast<int32_t>(min(static_cast<int64_t>(bl.count - st.block), st.end - (st.at + kTileExtra + st.block)));
-        const RowsOut u{s.lo, s.n * group, st.tile * kTileRows, st.head, group};
+        const RowsOut u{s.lo, s.n * group.n, st.tile * kTileRows, st.head, group};
         const float c2 = in.scale * (E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f) * kLog2e;
         const float v_scale = E4M3 ? scalar_load(cache.v_scale + st.head) : 1.0f;
         // this lane's row, and the tokens of the wave's rows
         const int32_t row = u.row0 + wave * 32 + n32;
         const bool row_ok = row < u.n_rows;
-        const int32_t tok = min(row, u.n_rows - 1) / group;
+        const int32_t tok = group.div(min(row, u.n_rows - 1));
         const int32_t base = s.len - s.n;
         const int32_t pos = base + tok;  // (rows past the last repeat it and are not stored)
         const int32_t wrow0 = u.row0 + wave * 32;
         const bool wave_on = wrow0 < u.n_rows;
-        const int32_t p_first = base + min(wrow0, u.n_rows - 1) / group;
-        const int32_t p_last = base + min(wrow0 + 31, u.n_rows - 1) / group;
+        const int32_t p_first = base + group.div(min(wrow0, u.n_rows - 1));
+        const int32_t p_last = base + group.div(min(wrow0 + 31, u.n_rows - 1));
         bf16x8_t Q[kSteps];
         {
             const uint16_t* qr = in.q + (u.lo + tok) * in.q_stride +
-                                 static_cast<int64_t>(u.head * group + min(row, u.n_rows - 1) % group) * HD;
+                                 static_cast<int64_t>(u.head * group.n + min(row, u.n_rows - 1) - tok * group.n) * HD;
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
                 const int c = E4M3 ? 4 * (i >> 1) + 2 * half + (i & 1) : 2 * i + half;
@@ -659,7 +671,7 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
                 __syncthreads();
                 const int r = tid % kTileRows;
                 notes.note(tid / kTileRows, r,
-                           seen_keys(key0, base + min(u.row0 + r, u.n_rows - 1) / group, in.window, gone),
+                           seen_keys(key0, base + group.div(min(u.row0 + r, u.n_rows - 1)), in.window, gone),
                            odd_keys);
             }
             if (!wave_on || key0 > p_last) return;
@@ -881,7 +893,7 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
     if (st.at >= st.end) return;
     const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, n16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int32_t group = in.n_q / cache.n_kv;
+    const HeadGroup group = in.group;
     int unit = 0;
     if (tid == 0) odd_unit = -1;
     __syncthreads();
@@ -906,7 +918,7 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
         const Blocks bl = blocks_of(s, 0, group, M, in.window);
         const int32_t count =
             static_cast<int32_t>(min(static_cast<int64_t>(bl.count - st.block), st.end - (st.at + kRowExtra + st.block)));
-        const RowsOut u{s.lo, s.n * group, 0, st.head, group};
+        const RowsOut u{s.lo, s.n * group.n, 0, st.head, group};
         const float c2 = in.scale * (E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f) * kLog2e;
         const int32_t base = s.len - s.n;
         const int32_t p_first = base, p_last = s.len - 1;
@@ -914,10 +926,10 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
         bf16x8_t Q[NB][kSteps];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            const int32_t row = 16 * b + n16, held = min(row, u.n_rows - 1), tok = held / group;
+            const int32_t row = 16 * b + n16, held = min(row, u.n_rows - 1), tok = group.div(held);
             pos[b] = base + tok;  // (rows past the last repeat it and are not stored)
             const uint16_t* qr = in.q + (u.lo + tok) * in.q_stride +
-                                 static_cast<int64_t>(u.head * group + held % group) * HD;
+                                 static_cast<int64_t>(u.head * group.n + held - tok * group.n) * HD;
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
                 const int c = E4M3 ? 8 * (i >> 1) + 2 * g4 + (i & 1) : 4 * i + g4;
@@ -983,7 +995,7 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
                 __builtin_amdgcn_s_waitcnt(0);
                 if (lane < 2 * M)
                     notes.note(lane / M, lane % M,
-                               seen_keys(key0, base + min(lane % M, u.n_rows - 1) / group, in.window, gone),
+                               seen_keys(key0, base + group.div(min(lane % M, u.n_rows - 1)), in.window, gone),
                                odd_keys[wave]);
             }
             f32x4_t S[NB][kGroups];

@@ -200,6 +200,18 @@ hipError_t launch_kv_append(const void* k, int64_t k_stride, const void* v, int6
                             const int32_t* T_valid, const RopeIn& rope, const KvCacheIn& cache,
                             bool e4m3, uint32_t* err_word, hipStream_t stream);
 
+// Query heads per key head, and how to divide by them: by a multiplication where that
+// is exact (x n < 2^32 for every x that occurs), mul = floor(2^32 / n) + 1.
+struct HeadGroup {
+    int32_t n;
+    uint32_t mul;  // 0: by a division
+#ifdef __HIPCC__
+    __device__ __forceinline__ int32_t div(int32_t x) const {
+        if (mul) return static_cast<int32_t>(__umulhi(static_cast<uint32_t>(x), mul));
+        return n == 1 ? x : x / n;
+    }
+#endif
+};
 // One attention call: rows of queries over the pages of their requests.
 struct AttendIn {
     const uint16_t* q;
@@ -212,6 +224,7 @@ struct AttendIn {
     uint32_t* err_word;
     int32_t n_q, T_max, window, max_q;
     float scale;
+    HeadGroup group;
 };
 size_t attend_workspace(int32_t n_q, int32_t max_q, const KvCacheIn& cache);
 hipError_t launch_attend(const AttendIn& in, const KvCacheIn& cache, bool e4m3, void* ws,
