@@ -151,23 +151,26 @@ __device__ __forceinline__ int64_t wave_sum64(int64_t v) {
     return v;
 }
 
-// One workgroup.  Blocks of each request (a thread each, or where a request has
-// many tiles a wave each), their prefix, then the start of every range by a search
-// in the prefix and a walk over the request's tiles.  A range that would begin inside
+// Blocks of each request, their prefix, then the start of every range by a search in
+// the prefix and among the request's tiles.  Where a request has few tiles, one
+// workgroup with a thread a request and a thread a range; where it may have MANY, a
+// wave each, and as many workgroups as there are ranges for (all find the same
+// prefix): walking over 64 tiles a thread took 25 us on the one CU.  A range that would begin inside
 // a short unit (up to `whole` blocks) begins at the nearer end of it
 // instead: in the tile kernel a cut unit costs its parts' way through memory, 64 KB
 // each, and sixteen prompts of 128 to 1024 tokens take 245 us with every end cut and
 // 195 so.
+template <bool MANY>
 __global__ void __launch_bounds__(kPlanThreads)
 attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int32_t n_wg,
-                   int32_t least, int32_t whole, int32_t extra, int32_t many) {
+                   int32_t least, int32_t whole, int32_t extra) {
     __shared__ int64_t upto[kMaxRequests + 1], begins[kMaxRanges + 1];
     __shared__ int64_t wave_total[kPlanThreads / kWave];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int32_t R = cache.R_max;
     const HeadGroup group = in.group;
     bool bad = false;
-    if (!many) {
+    if constexpr (!MANY) {
         for (int32_t r = tid; r < R; r += kPlanThreads) {
             const Span s = span_of(in, cache, r, &bad);
             const int32_t tiles = tiles_of(s.n, group, rows);
@@ -186,7 +189,7 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
             if (lane == 0) upto[r + 1] = sum * cache.n_kv;
         }
     }
-    if (bad) atomicOr(in.err_word, kErrKvSpan);
+    if (bad && blockIdx.x == 0) atomicOr(in.err_word, kErrKvSpan);
     if (tid == 0) upto[0] = 0;
     __syncthreads();
     // prefix over the requests, four to a thread
@@ -211,7 +214,7 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
     __syncthreads();
     const int64_t blocks = upto[R];
     const int64_t share = max(static_cast<int64_t>(least), (blocks + n_wg - 1) / n_wg);
-    // the unit and its block at position `at`, and the unit's blocks
+    // The unit and its block at position `at` (uniform where MANY), and the unit's blocks.
     auto locate = [&](int64_t at, int32_t* count) {
         int32_t lo = 0, hi = R - 1;  // the last request that starts at or before `at`
         while (lo < hi) {
@@ -223,23 +226,40 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
         const int64_t a_head = (upto[lo + 1] - upto[lo]) / cache.n_kv, rest = at - upto[lo];
         WorkRange st{at, 0, share, lo, static_cast<int32_t>(rest / a_head), 0, 0, s.lo, s.n, s.len, 0};
         int64_t left = rest % a_head;
-        for (;;) {
-            *count = blocks_of(s, st.tile, group, rows, in.window).count;
-            if (left < *count + extra) break;
-            left -= *count + extra;
-            ++st.tile;
+        const int32_t tiles = tiles_of(s.n, group, rows);
+        *count = 1;
+        if constexpr (MANY) {  // 64 tiles at a time
+            for (; st.tile < tiles; st.tile += kWave) {
+                const int32_t t = st.tile + lane;
+                const int32_t mine = t < tiles ? blocks_of(s, t, group, rows, in.window).count : 0;
+                int64_t incl = t < tiles ? mine + extra : 0;
+                for (int o = 1; o < kWave; o <<= 1) {
+                    const int64_t up = __shfl_up(incl, o);
+                    if (lane >= o) incl += up;
+                }
+                const uint64_t beyond = wave_ballot(incl > left);
+                if (beyond) {
+                    const int first = __builtin_ctzll(beyond);
+                    if (first > 0) left -= __shfl(incl, first - 1);
+                    *count = __shfl(mine, first);
+                    st.tile += first;
+                    break;
+                }
+                left -= __shfl(incl, kWave - 1);
+            }
+        } else {
+            for (; st.tile < tiles; ++st.tile) {
+                *count = blocks_of(s, st.tile, group, rows, in.window).count;
+                if (left < *count + extra) break;
+                left -= *count + extra;
+            }
         }
         st.at -= left;  // the unit's own
         st.block = static_cast<int32_t>(max(static_cast<int64_t>(0), left - extra));
         return st;
     };
-    // The workgroups are dealt over the XCDs in turn; neighbouring ranges, which read
-    // the same keys, go to one XCD and its L2, and few ranges still to all of them.
-    const int32_t used = static_cast<int32_t>(min(static_cast<int64_t>(n_wg), (blocks + share - 1) / share));
-    const int32_t each = (used + 7) / 8;
-    const int32_t w = tid;  // (a thread per range)
-    WorkRange st{blocks, 0, share, 0, 0, 0, 0, 0, 0, 0, 0};
-    if (w <= n_wg) {
+    auto begin_of = [&](int32_t w) {
+        WorkRange st{blocks, 0, share, 0, 0, 0, 0, 0, 0, 0, 0};
         int32_t count;
         if (w * share < blocks) {
             st = locate(w * share, &count);
@@ -250,16 +270,43 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
                 if (next && st.at < blocks) st = locate(st.at, &count);
             }
         }
-        begins[w] = st.at + (st.block ? extra + st.block : 0);
-    }
-    __syncthreads();
-    if (w < n_wg) {
+        return st;
+    };
+    // The workgroups are dealt over the XCDs in turn; neighbouring ranges, which read
+    // the same keys, go to one XCD and its L2, and few ranges still to all of them.
+    const int32_t used = static_cast<int32_t>(min(static_cast<int64_t>(n_wg), (blocks + share - 1) / share));
+    const int32_t each = (used + 7) / 8;
+    // this workgroup's ranges, and where the one behind them begins
+    const int32_t per = n_wg / gridDim.x, w0 = blockIdx.x * per;
+    auto note_begin = [&](int32_t i, const WorkRange& st) {
+        begins[i] = st.at + (st.block ? extra + st.block : 0);
+    };
+    auto put_range = [&](int32_t i, WorkRange st) {
+        const int32_t w = w0 + i;
         ws.done[w] = 0;
-        st.end = begins[w + 1];
-        if (begins[w] == st.end) st.end = st.at;  // nothing to do
+        st.end = begins[i + 1];
+        if (begins[i] == st.end) st.end = st.at;  // nothing to do
         st.nth = w;
         // range w at each * (b % 8) + b / 8; the others behind them, in order
         ws.range[w < 8 * each ? w / each + 8 * (w % each) : w] = st;
+    };
+    if constexpr (MANY) {  // a wave a range
+        const WorkRange st = begin_of(w0 + wave);
+        if (lane == 0) note_begin(wave, st);
+        if (wave == 0) {
+            const WorkRange last = begin_of(w0 + per);
+            if (lane == 0) note_begin(per, last);
+        }
+        __syncthreads();
+        if (lane == 0) put_range(wave, st);
+    } else {  // a thread a range
+        WorkRange st;
+        if (tid <= per) {
+            st = begin_of(w0 + tid);
+            note_begin(tid, st);
+        }
+        __syncthreads();
+        if (tid < per) put_range(tid, st);
     }
 }
 
@@ -865,7 +912,7 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
                 st.head = 0;
                 if (st.at < st.end)
                     do ++st.req;
-                    while (scalar_span(in, cache, st.req).n == 0);
+                    while (st.req < cache.R_max - 1 && scalar_span(in, cache, st.req).n == 0);
             }
         }
     }
@@ -1204,7 +1251,7 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
             st.head = 0;
             if (st.at < st.end)
                 do ++st.req;
-                while (scalar_span(in, cache, st.req).n == 0);
+                while (st.req < cache.R_max - 1 && scalar_span(in, cache, st.req).n == 0);
         }
     }
 }
@@ -1263,9 +1310,14 @@ hipError_t launch_attend(const AttendIn& in, const KvCacheIn& cache, bool e4m3, 
     const AttendWs aw{reinterpret_cast<WorkRange*>(p), reinterpret_cast<int32_t*>(p + w.done),
                       reinterpret_cast<float*>(p + w.parts)};
     const int64_t most = (static_cast<int64_t>(in.max_q) * (in.n_q / cache.n_kv) + rows - 1) / rows;
-    hipLaunchKernelGGL(attend_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, in, cache, aw, rows,
-                       n_wg, rows == kTileRows ? 1 : 4, rows == kTileRows ? kWholeUnit : 0,
-                       rows == kTileRows ? kTileExtra : kRowExtra, most > 4 ? 1 : 0);
+    const int32_t least = rows == kTileRows ? 1 : 4, whole = rows == kTileRows ? kWholeUnit : 0;
+    const int32_t extra = rows == kTileRows ? kTileExtra : kRowExtra;
+    if (most > 4)
+        hipLaunchKernelGGL(attend_plan_kernel<true>, dim3(n_wg / (kPlanThreads / kWave)), dim3(kPlanThreads), 0,
+                           stream, in, cache, aw, rows, n_wg, least, whole, extra);
+    else
+        hipLaunchKernelGGL(attend_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, stream, in, cache, aw,
+                           rows, n_wg, least, whole, extra);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel_for(cache.head_dim, e4m3, rows), dim3(n_wg), dim3(kAttendThreads), 0, stream,
@@ -1274,7 +1326,8 @@ hipError_t launch_attend(const AttendIn& in, const KvCacheIn& cache, bool e4m3, 
 }
 
 void add_attend_kernels(std::vector<KernelInfo>& t) {
-    t.push_back(kernel_info(attend_plan_kernel));
+    t.push_back(kernel_info(attend_plan_kernel<false>));
+    t.push_back(kernel_info(attend_plan_kernel<true>));
     for (const auto& width : kKernels)
         for (const auto& type : width)
             for (const AttendKernel k : type) t.push_back(kernel_info(k));
