@@ -5,6 +5,10 @@ parameters, the batch's request layout and subscriptions) into device
 buffers of static shape and runs the step through the C ABI, in this
 order for every layer:
 
+  0. where the layer has an attention (an attention hook): its heads normed and
+     rotated, the step's keys and values appended to the layer's paged cache, and the
+     attention of the batch's tokens over it, whose output is the activation that
+     the rest reads and writes;
   1. route build (once per step: the batch and subscriptions are shared by
      all hooked layers; when the first layer's first consumer of the routing
      is an SAE encode, or its fused probes + steering pass, that kernel
@@ -31,9 +35,10 @@ from typing import List, Optional
 import numpy as np
 import torch
 
-from . import (XMIX_PROBE_LAST, XMIX_PROBE_MEAN, XMIX_PROBE_TOKEN, Ring, Route, SaeApp, SaeDict,
-               probe_workspace, sae_encode_workspace, xmix_probe_score, xmix_readback_compact,
-               xmix_route_build, xmix_route_sae_encode_topk_multi, xmix_sae_clamp_decode,
+from . import (XMIX_PROBE_LAST, XMIX_PROBE_MEAN, XMIX_PROBE_TOKEN, KvCache, Ring, Rope, Route,
+               SaeApp, SaeDict, paged_attention_workspace, probe_workspace, sae_encode_workspace,
+               xmix_kv_append, xmix_paged_attention, xmix_probe_score, xmix_qk_norm_rope,
+               xmix_readback_compact, xmix_route_build, xmix_route_sae_encode_topk_multi, xmix_sae_clamp_decode,
                xmix_sae_clamp_decode_multi, xmix_sae_encode_candidates,
                xmix_sae_encode_topk, xmix_sae_encode_topk_multi, xmix_sae_encode_topk_ring,
                xmix_sae_fold_bias, xmix_route_sae_encode_candidates, xmix_route_steer_probe,
@@ -84,10 +89,27 @@ class _Sae:
 
 
 @dataclass
+class _Attention:
+    q: torch.Tensor          # parts of the projections' output, [T_max, heads, head_dim]
+    k: torch.Tensor
+    v: torch.Tensor
+    q_rot: torch.Tensor      # normed and rotated
+    k_rot: Optional[torch.Tensor]   # None: the append rotates the keys
+    q_weight: Optional[torch.Tensor]
+    k_weight: Optional[torch.Tensor]
+    eps: float
+    rope: Rope
+    cache: KvCache
+    window: int
+    out: torch.Tensor        # the layer's h as heads
+
+
+@dataclass
 class _Layer:
     layer_id: int
     h_in: torch.Tensor
     h: torch.Tensor
+    attention: Optional[_Attention] = None
     steer_v: Optional[torch.Tensor] = None
     steer_bits: List[int] = field(default_factory=list)
     probes: List[_Probes] = field(default_factory=list)
@@ -117,10 +139,22 @@ class HookStep:
         self.err = torch.zeros(1, dtype=torch.int32, device=dev)
         self.cu = None if wl.cu_seqlens is None else to_device(wl.cu_seqlens, torch.int32, dev)
         self.route = Route(wl.T_max, wl.n_apps, dev)
+        self.kv_len = self.pos = self.attention_ws = None
+        if wl.ctx is not None:
+            # a token's position: what its request has cached before the step, and its
+            # place in the span; -1 for padding, as in the request ids
+            self.kv_len = to_device(wl.ctx + np.diff(wl.cu_seqlens), torch.int32, dev)
+            on = (wl.req >= 0) & (np.arange(wl.T_max) < wl.T_valid)
+            r = np.where(on, wl.req, 0)
+            self.pos = to_device(np.where(on, wl.ctx[r] + np.arange(wl.T_max) - wl.cu_seqlens[r], -1),
+                                 torch.int32, dev)
+            self.max_q = max(int(np.diff(wl.cu_seqlens).max()), 1)
         self.layers: List[_Layer] = []
         for L in wl.layers:
             h_in = to_device(L.h, act, dev)
             lay = _Layer(L.layer_id, h_in, h_in.clone())
+            if L.attention is not None:
+                lay.attention = self._attention(L.attention, lay.h)
             if L.steer:
                 lay.steer_v = to_device(np.stack([s.v for s in L.steer]), act, dev)
                 lay.steer_bits = [s.bit for s in L.steer]
@@ -162,6 +196,23 @@ class HookStep:
                     sae.ring = Ring(s.ring_capacity, 16 + s.k * 4 + s.k * 2, dev)
                 lay.saes.append(sae)
             self.layers.append(lay)
+
+    def _attention(self, a, h) -> _Attention:
+        dev = self.device
+        qkv = to_device_bits(a.qkv, dev)
+        q, k, v = qkv.split((a.n_q, a.n_kv, a.n_kv), dim=1)
+        w = [None if x is None else to_device_bits(x, dev) for x in (a.q_weight, a.k_weight)]
+        cache = KvCache(to_device_bits(a.k_pages, dev), to_device_bits(a.v_pages, dev),
+                        to_device(a.pages, torch.int32, dev))
+        # normed keys are normed and rotated with the queries, others rotated by the append
+        k_rot = None if w[1] is None else torch.empty((k.shape), dtype=k.dtype, device=dev)
+        need = paged_attention_workspace(h.shape[0], a.n_q, self.max_q, cache)
+        if self.attention_ws is None or self.attention_ws.numel() < need:
+            # one for all layers, which follow each other
+            self.attention_ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        return _Attention(q, k, v, torch.empty(q.shape, dtype=q.dtype, device=dev), k_rot, w[0], w[1],
+                          a.eps, Rope(to_device(a.inv_freq, torch.float64, dev)), cache, a.window,
+                          h.view(h.shape[0], a.n_q, a.head_dim))
 
     def reset(self):
         """Restore every layer's activation to its input value."""
@@ -210,6 +261,17 @@ class HookStep:
                                                     self.err, stream))
         modes = {XMIX_PROBE_TOKEN: "token", XMIX_PROBE_MEAN: "mean", XMIX_PROBE_LAST: "last"}
         for li, lay in enumerate(self.layers):
+            if lay.attention is not None:
+                a = lay.attention
+                issue(f"L{li}/norm_rope", lambda a=a: xmix_qk_norm_rope(
+                    a.q, None if a.k_rot is None else a.k, self.pos, a.q_weight, a.k_weight, a.eps,
+                    a.rope, a.q_rot, a.k_rot, stream=stream))
+                issue(f"L{li}/kv_append", lambda a=a: xmix_kv_append(
+                    a.k if a.k_rot is None else a.k_rot, a.v, self.req, self.pos,
+                    a.rope if a.k_rot is None else None, a.cache, self.err, stream=stream))
+                issue(f"L{li}/attention", lambda a=a: xmix_paged_attention(
+                    a.q_rot, self.cu, self.kv_len, a.cache, a.q.shape[2] ** -0.5, a.window,
+                    self.max_q, a.out, None, self.err, self.attention_ws, stream=stream))
             fused = None  # the token probes that run in one pass with the steering
             if self.fuse_steer_probe and lay.steer_v is not None:
                 fused = next((p for p in lay.probes if p.mode == XMIX_PROBE_TOKEN), None)
@@ -321,6 +383,13 @@ class HookStep:
         live[ok] = sub[wl.req[ok]]
         total = 0
         for L in wl.layers:
+            if L.attention is not None:
+                a, n = L.attention, np.diff(wl.cu_seqlens)
+                # projections read; queries written and read; keys and values stored, and
+                # read with what is cached (of a window, what its tokens see); the output
+                seen = wl.ctx + n if not a.window else np.minimum(wl.ctx + n, a.window + n - 1)
+                total += int(n.sum()) * a.head_dim * 2 * (4 * a.n_q + 4 * a.n_kv)
+                total += int(seen[n > 0].sum()) * 2 * a.n_kv * a.head_dim * 2
             steer_bits = sum(1 << s.bit for s in L.steer)
             read_bits = steer_bits | sum(1 << p.bit for p in L.probes) | sum(1 << s.bit for s in L.saes)
             rows_read = int(np.count_nonzero(live & np.uint64(read_bits)))

@@ -176,12 +176,30 @@ class SaeApp:
 
 
 @dataclass
+class Attention:
+    """The attention that makes a layer's activation (h: its heads side by side)."""
+    n_q: int
+    n_kv: int
+    head_dim: int
+    qkv: np.ndarray          # [T_max, n_q + 2 n_kv, head_dim] bf16 bits, the projections' output
+    k_pages: np.ndarray      # [n_pages, n_kv, page_size, head_dim] bf16 bits: what is cached
+    v_pages: np.ndarray
+    pages: np.ndarray        # int32 [R_max, max_pages]
+    inv_freq: np.ndarray     # float64 [rot_dim / 2]
+    q_weight: Optional[np.ndarray] = None   # [head_dim] bf16 bits; None: heads are not normed
+    k_weight: Optional[np.ndarray] = None
+    eps: float = 1e-6
+    window: int = 0
+
+
+@dataclass
 class Layer:
     layer_id: int
     h: np.ndarray            # [T_max, d] bf16 bits or float32
     steer: List[SteerApp] = field(default_factory=list)
     probes: List[ProbeApp] = field(default_factory=list)
     saes: List[SaeApp] = field(default_factory=list)
+    attention: Optional[Attention] = None
 
 
 @dataclass
@@ -198,6 +216,7 @@ class Workload:
     alpha: np.ndarray        # float32 [R_max, n_steer], shared by all layers
     layers: List[Layer]
     cu_seqlens: Optional[np.ndarray] = None   # int32 [R_max + 1]
+    ctx: Optional[np.ndarray] = None          # int32 [R_max]: tokens cached before the step
     description: str = ""
 
     @property
@@ -373,6 +392,40 @@ def make_c5(seed=0, d=8192, T=512, m=65536, k=64, p=0.2, n_steer=16, n_probe=8, 
     return Workload(cfg, "bf16", d, T, T, R, n_apps, req, sub, alpha,
                     [Layer(0, h, steer, probes, saes)],
                     description=f"decode d={d} T=R={T} apps={n_apps} m={m} k={k}")
+
+
+def with_attention(wl, n_q, n_kv, ctx_lo=0, ctx_hi=64, page_size=16, rot_dim=None, norm=True,
+                   window=0, theta=500000.0, seed=0):
+    """The workload `wl` with an attention in front of every layer's hook, which makes
+    the layer's activation: d = n_q heads side by side, ctx_lo to ctx_hi cached
+    tokens a request in pages of no order, the first rot_dim values of a head rotated
+    (None: all), heads normed or not."""
+    hd, R, T = wl.d // n_q, wl.R_max, wl.T_max
+    if hd * n_q != wl.d or wl.dtype != "bf16":
+        raise ValueError("attention needs a bf16 activation of n_q whole heads")
+    cfg = f"{wl.name}/attention"
+    if wl.cu_seqlens is None:  # one token per request, in order
+        wl.cu_seqlens = np.minimum(np.arange(R + 1), wl.T_valid).astype(np.int32)
+    wl.ctx = randint(f"{cfg}/ctx", R, ctx_lo, ctx_hi, seed).astype(np.int32)
+    count = -(-(wl.ctx + np.diff(wl.cu_seqlens)) // page_size)
+    order = permutation(f"{cfg}/pages", int(count.sum()) + 2, seed)
+    pages = np.full((R, max(int(count.max()), 1)), -1, dtype=np.int32)
+    at = np.concatenate([[0], np.cumsum(count)])
+    for r in range(R):
+        pages[r, :count[r]] = order[at[r]:at[r + 1]]
+    rot = hd if rot_dim is None else rot_dim
+    inv_freq = theta ** (-np.arange(0, rot, 2, dtype=np.float64) / rot)
+    shape = (len(order), n_kv, page_size, hd)
+    for L in wl.layers:
+        tag = f"{cfg}/L{L.layer_id}"
+        w = [normal_bf16(f"{tag}/{x}_weight", (hd,), 0.2, mean=1.0, seed=seed) if norm else None
+             for x in "qk"]
+        L.attention = Attention(
+            n_q, n_kv, hd, normal_bf16(f"{tag}/qkv", (T, n_q + 2 * n_kv, hd), 1.0, seed=seed),
+            normal_bf16(f"{tag}/k_pages", shape, 1.0, seed=seed),
+            normal_bf16(f"{tag}/v_pages", shape, 1.0, seed=seed), pages, inv_freq, w[0], w[1],
+            window=window)
+    return wl
 
 
 MAKERS = {"c1": make_c1, "c2": make_c2, "c3": make_c3, "c4": make_c4, "c5": make_c5}
