@@ -14,16 +14,18 @@
 // V^T is read from LDS by the transposing reads (ds_read_tr).
 //
 // Work is dealt in blocks of 64 keys.  A unit is one key head of one request and a
-// tile of its rows; the blocks of all units, one behind the other, are cut into equal
-// ranges, one per workgroup, whatever the lengths are.  A unit that is cut leaves a
+// tile of its rows; the blocks of all units, one behind the other and weighed by what
+// they cost, are cut into equal ranges, one per workgroup, whatever the lengths are.  A unit that is cut leaves a
 // part (maximum, sum, O) per workgroup in the workspace, and the last workgroup to
 // finish one joins them in order.  attend_plan_kernel finds where each range starts.
 //
-// Two forms of the inner loop:
-//   tile kernel   128 rows a unit; the workgroup's four waves take 32 rows each and
-//                 share K and V in LDS (chunks of a prompt, mixed batches)
-//   row kernel    16 or 32 rows a unit; the waves take keys of their own (decode and
-//                 drafted tokens, where the cache is read once and memory is the bound)
+// Two kinds of unit, each with an inner loop of its own:
+//   tile unit   128 rows; the workgroup's four waves take 32 rows each and share K
+//               and V in LDS (chunks of a prompt: the matrix units are the bound)
+//   row unit    16 or 32 rows; the waves take keys of their own (decode and drafted
+//               tokens, where the cache is read once and memory is the bound)
+// A launch whose requests all have few rows is of row units alone; in any other, the
+// requests that do have few go as row units among the tiles.
 #include "common.hpp"
 #include "kernels.hpp"
 #include "launch.hpp"
@@ -50,10 +52,10 @@ typedef int i32x2_t __attribute__((ext_vector_type(2)));
 constexpr int kAttendThreads = 256, kAttendWaves = 4;
 constexpr int kBlockKeys = 64;     // keys of a block
 constexpr int kGroupKeys = 16;     // keys that surely lie in one page
-constexpr int kTileRows = 128;     // rows of a unit of the tile kernel
+constexpr int kTileRows = 128;     // rows of a tile unit
+constexpr int kFewRows = 16;       // rows of a request that are a row unit among tiles
 constexpr int kMaxRequests = 4096, kMaxRanges = 512;
 constexpr int kPlanThreads = 1024;
-constexpr int kWholeUnit = 18;    // units of so many blocks are not cut (tile kernel)
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 // A running maximum is raised only by a score this far above it (powers of two): the
 // weights stay below 2^8, which neither fp32 sums nor bf16 weights mind, and the
@@ -70,9 +72,24 @@ struct WorkRange {
     int32_t lo, n, len;              // the request's span and keys
     int32_t nth;                     // its place among the ranges
 };
-// What a unit costs beside its blocks (its queries, the first copies, its rows), in
-// blocks: ranges of units of one block each took three times as long as others.
-constexpr int kTileExtra = 3, kRowExtra = 4;
+// What is dealt: a unit's place is `extra` for what it costs beside its blocks (its
+// queries, the first copies, its rows), then `step` for each block (`few_step` where
+// a request of a launch of tiles has few rows).
+struct Deal {
+    int32_t rows;                   // of a unit
+    int32_t extra, step, few_step;
+    int32_t least;                  // places of a range, at least a step: no range between
+                                    // the first and the last of a unit is without a block
+    int32_t whole;                  // tiles of so many blocks are not cut
+};
+// A block of a tile takes half as long again as one of a row unit (1.4 us and 0.9 us
+// at head_dim 64, two workgroups on a CU), a unit's own cost is 4 to 8 us.
+constexpr Deal kDealRows = {0, 4, 1, 1, 4, 0}, kDealTiles = {kTileRows, 9, 3, 2, 3, 18};
+__host__ __device__ constexpr Deal deal_of(int32_t rows) {
+    Deal d = rows == kTileRows ? kDealTiles : kDealRows;
+    d.rows = rows;
+    return d;
+}
 // The workspace: a range per workgroup, a count of finished parts per range that
 // begins a cut unit, and two parts per range.
 struct AttendWs {
@@ -126,6 +143,8 @@ __device__ __forceinline__ Span scalar_span(const AttendIn& in, const KvCacheIn&
 // A uniform value in a scalar register, where the compiler has put it in a vector one
 // (a resource made of it would be rebuilt lane by lane).
 __device__ __forceinline__ int32_t scalar(int32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+// A request whose rows are a row unit's in a launch of tiles.
+__device__ __forceinline__ bool few_rows(int32_t n, const HeadGroup& group) { return n * group.n <= kFewRows; }
 __device__ __forceinline__ int32_t tiles_of(int32_t n, const HeadGroup& group, int32_t rows) {
     return static_cast<int32_t>((static_cast<uint32_t>(n) * group.n + rows - 1) / rows);
 }
@@ -155,36 +174,37 @@ __device__ __forceinline__ int64_t wave_sum64(int64_t v) {
 // the prefix and among the request's tiles.  Where a request has few tiles, one
 // workgroup with a thread a request and a thread a range; where it may have MANY, a
 // wave each, and as many workgroups as there are ranges for (all find the same
-// prefix): walking over 64 tiles a thread took 25 us on the one CU.  A range that would begin inside
-// a short unit (up to `whole` blocks) begins at the nearer end of it
-// instead: in the tile kernel a cut unit costs its parts' way through memory, 64 KB
-// each, and sixteen prompts of 128 to 1024 tokens take 245 us with every end cut and
-// 195 so.
+// prefix): walking over 64 tiles a thread took 25 us on the one CU.  A range that would
+// begin inside a short tile unit (up to `whole` blocks) begins at the nearer end of it
+// instead: its parts would take their way through memory, 64 KB each, and sixteen
+// prompts of 128 to 1024 tokens took 245 us with every end cut and 211 so.
 template <bool MANY>
 __global__ void __launch_bounds__(kPlanThreads)
-attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int32_t n_wg,
-                   int32_t least, int32_t whole, int32_t extra) {
+attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t n_wg) {
     __shared__ int64_t upto[kMaxRequests + 1], begins[kMaxRanges + 1];
     __shared__ int64_t wave_total[kPlanThreads / kWave];
+    __shared__ uint64_t tile_ranges[kMaxRanges / kWave];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int32_t R = cache.R_max;
     const HeadGroup group = in.group;
+    const int32_t rows = deal.rows, extra = deal.extra;
+    auto step_of = [&](int32_t n) { return few_rows(n, group) ? deal.few_step : deal.step; };
     bool bad = false;
     if constexpr (!MANY) {
         for (int32_t r = tid; r < R; r += kPlanThreads) {
             const Span s = span_of(in, cache, r, &bad);
-            const int32_t tiles = tiles_of(s.n, group, rows);
+            const int32_t tiles = tiles_of(s.n, group, rows), step = step_of(s.n);
             int64_t sum = 0;
-            for (int32_t t = 0; t < tiles; ++t) sum += blocks_of(s, t, group, rows, in.window).count + extra;
+            for (int32_t t = 0; t < tiles; ++t) sum += blocks_of(s, t, group, rows, in.window).count * step + extra;
             upto[r + 1] = sum * cache.n_kv;
         }
     } else {
         for (int32_t r = wave; r < R; r += kPlanThreads / kWave) {
             const Span s = span_of(in, cache, r, &bad);
-            const int32_t tiles = tiles_of(s.n, group, rows);
+            const int32_t tiles = tiles_of(s.n, group, rows), step = step_of(s.n);
             int64_t sum = 0;
             for (int32_t t = lane; t < tiles; t += kWave)
-                sum += blocks_of(s, t, group, rows, in.window).count + extra;
+                sum += blocks_of(s, t, group, rows, in.window).count * step + extra;
             sum = wave_sum64(sum);
             if (lane == 0) upto[r + 1] = sum * cache.n_kv;
         }
@@ -212,27 +232,32 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
     for (int i = 0; i < kEach; ++i)
         if (tid * kEach + i < R) upto[tid * kEach + i + 1] = before + v[i];
     __syncthreads();
-    const int64_t blocks = upto[R];
-    const int64_t share = max(static_cast<int64_t>(least), (blocks + n_wg - 1) / n_wg);
-    // The unit and its block at position `at` (uniform where MANY), and the unit's blocks.
-    auto locate = [&](int64_t at, int32_t* count) {
-        int32_t lo = 0, hi = R - 1;  // the last request that starts at or before `at`
+    const int64_t places = upto[R];
+    const int64_t share = max(static_cast<int64_t>(deal.least), (places + n_wg - 1) / n_wg);
+    // The last request that starts at or before a place.
+    auto request_at = [&](int64_t at) {
+        int32_t lo = 0, hi = R - 1;
         while (lo < hi) {
             const int32_t mid = (lo + hi + 1) >> 1;
             if (upto[mid] <= at) lo = mid;
             else hi = mid - 1;
         }
+        return lo;
+    };
+    // The unit and its block at position `at` (uniform where MANY), and the unit's blocks.
+    auto locate = [&](int64_t at, int32_t* count) {
+        const int32_t lo = request_at(at);
         const Span s = span_of(in, cache, lo);
         const int64_t a_head = (upto[lo + 1] - upto[lo]) / cache.n_kv, rest = at - upto[lo];
         WorkRange st{at, 0, share, lo, static_cast<int32_t>(rest / a_head), 0, 0, s.lo, s.n, s.len, 0};
         int64_t left = rest % a_head;
-        const int32_t tiles = tiles_of(s.n, group, rows);
+        const int32_t tiles = tiles_of(s.n, group, rows), step = step_of(s.n);
         *count = 1;
         if constexpr (MANY) {  // 64 tiles at a time
             for (; st.tile < tiles; st.tile += kWave) {
                 const int32_t t = st.tile + lane;
                 const int32_t mine = t < tiles ? blocks_of(s, t, group, rows, in.window).count : 0;
-                int64_t incl = t < tiles ? mine + extra : 0;
+                int64_t incl = t < tiles ? mine * step + extra : 0;
                 for (int o = 1; o < kWave; o <<= 1) {
                     const int64_t up = __shfl_up(incl, o);
                     if (lane >= o) incl += up;
@@ -250,36 +275,75 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
         } else {
             for (; st.tile < tiles; ++st.tile) {
                 *count = blocks_of(s, st.tile, group, rows, in.window).count;
-                if (left < *count + extra) break;
-                left -= *count + extra;
+                if (left < *count * step + extra) break;
+                left -= *count * step + extra;
             }
         }
         st.at -= left;  // the unit's own
-        st.block = static_cast<int32_t>(max(static_cast<int64_t>(0), left - extra));
+        st.block = (max(0, static_cast<int32_t>(left) - extra) + step - 1) / step;
         return st;
     };
     auto begin_of = [&](int32_t w) {
-        WorkRange st{blocks, 0, share, 0, 0, 0, 0, 0, 0, 0, 0};
+        WorkRange st{places, 0, share, 0, 0, 0, 0, 0, 0, 0, 0};
         int32_t count;
-        if (w * share < blocks) {
+        if (w * share < places) {
             st = locate(w * share, &count);
-            if (count <= whole && st.block != 0) {
+            const int32_t step = step_of(st.n);
+            const bool uncut = count <= deal.whole && !few_rows(st.n, group);
+            if (st.block == count || (uncut && st.block != 0)) {
                 const bool next = 2 * st.block > count;
                 st.block = 0;
-                if (next) st.at += count + extra;
-                if (next && st.at < blocks) st = locate(st.at, &count);
+                if (next) st.at += count * step + extra;
+                if (next && st.at < places) st = locate(st.at, &count);
             }
         }
         return st;
     };
-    // The workgroups are dealt over the XCDs in turn; neighbouring ranges, which read
-    // the same keys, go to one XCD and its L2, and few ranges still to all of them.
-    const int32_t used = static_cast<int32_t>(min(static_cast<int64_t>(n_wg), (blocks + share - 1) / share));
+    // The workgroups are dealt over the XCDs in turn, workgroup b to XCD b % 8.
+    // Neighbouring ranges, which read the same keys, go to one XCD and its L2, and few
+    // ranges still to all of them; but tiles, which keep the matrix units busy, and
+    // rows, which wait for memory, are spread over the XCDs each on their own, the
+    // tiles first, such that a CU, whose second workgroup is 32 behind its first, has
+    // both: 95 single tokens and a chunk of 1001 take 134 us so, 140 with the ranges
+    // in their order and 161 with the rows first.
+    const int32_t used = static_cast<int32_t>(min(static_cast<int64_t>(n_wg), (places + share - 1) / share));
     const int32_t each = (used + 7) / 8;
+    const bool mixed = deal.step != deal.few_step;
+    if (mixed) {
+        if (tid < kMaxRanges) {
+            bool tile = false;
+            if (tid < used) {
+                const int32_t r = request_at(tid * share);
+                tile = !few_rows(in.cu[r + 1] - in.cu[r], group);
+            }
+            const uint64_t mask = wave_ballot(tile);
+            if (lane == 0) tile_ranges[wave] = mask;
+        }
+        __syncthreads();
+    }
+    auto workgroup_of = [&](int32_t w) {
+        if (w >= 8 * each) return w;
+        if (!mixed) return w / each + 8 * (w % each);
+        int32_t before = 0, all = 0;  // ranges of tiles
+        for (int32_t i = 0; i < kMaxRanges / kWave; ++i) {
+            const uint64_t mask = tile_ranges[i];
+            all += __popcll(mask);
+            const int32_t n = min(max(w - i * kWave, 0), kWave);
+            before += __popcll(n == kWave ? mask : mask & ((1ull << n) - 1));
+        }
+        const bool tile = (tile_ranges[w / kWave] >> (w % kWave)) & 1u;
+        for (int32_t x = 0;; ++x) {  // XCD x: `each` ranges, of them an eighth of the tiles
+            const int32_t t0 = x * all / 8, t1 = (x + 1) * all / 8;
+            const int32_t at = tile ? before - t0 : w - before - (x * each - t0);
+            const int32_t n = tile ? t1 - t0 : each - (t1 - t0);
+            if (at < n || x == 7) return x + 8 * (tile ? at : t1 - t0 + at);
+        }
+    };
     // this workgroup's ranges, and where the one behind them begins
     const int32_t per = n_wg / gridDim.x, w0 = blockIdx.x * per;
     auto note_begin = [&](int32_t i, const WorkRange& st) {
-        begins[i] = st.at + (st.block ? extra + st.block : 0);
+        const int32_t step = step_of(st.n);
+        begins[i] = st.at + (st.block ? extra + st.block * step : 0);
     };
     auto put_range = [&](int32_t i, WorkRange st) {
         const int32_t w = w0 + i;
@@ -287,8 +351,7 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
         st.end = begins[i + 1];
         if (begins[i] == st.end) st.end = st.at;  // nothing to do
         st.nth = w;
-        // range w at each * (b % 8) + b / 8; the others behind them, in order
-        ws.range[w < 8 * each ? w / each + 8 * (w % each) : w] = st;
+        ws.range[workgroup_of(w)] = st;
     };
     if constexpr (MANY) {  // a wave a range
         const WorkRange st = begin_of(w0 + wave);
@@ -315,9 +378,9 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, int32_t rows, int3
 // Rows of one head of the cache in LDS: how the 16-byte pieces of a row are permuted
 // (the copies into LDS place each piece linearly, so it is the source address that
 // is permuted), such that the lanes of one read cover all banks.
-//   K (both kernels): 16 lanes read one piece each of 16 rows
+//   K (both kinds): 16 lanes read one piece each of 16 rows
 //   V: the transposing reads take 4 rows of 32 bytes (bf16) or 8 of 16 bytes (e4m3)
-//   per 16 lanes; which rows and columns 32 lanes take differs between the kernels
+//   per 16 lanes; which rows and columns 32 lanes take differs between the kinds
 template <int RB>
 __device__ __forceinline__ int swz_k(int row) {
     constexpr int per = RB >= 256 ? 1 : 256 / RB, mask = RB >= 256 ? 15 : RB / 16 - 1;
@@ -509,14 +572,15 @@ __device__ __forceinline__ f32x4_t load4_through(__amdgpu_buffer_rsrc_t r, int o
     return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, kThrough));
 }
 
-// A part: the rows' maxima (powers of two, -inf: no key) and sums, then O [row][HD].
+// A part: the rows' maxima (powers of two, -inf: no key) and sums, then O [row][HD],
+// with room for SLOT rows.
 // Parts pass between XCDs, whose L2 caches do not see each other's writes: they are
 // stored through to memory and loaded from there (sc1), which needs no fence.  An
 // agent fence writes the whole L2 back, a good half microsecond each, one
 // after the other: a call of 32 workgroups took 33 us with them and 10 without.
-template <int M, int HD>
+template <int M, int HD, int SLOT>
 struct Part {
-    static constexpr int kFloats = M * (HD + 2);
+    static constexpr int kFloats = SLOT * (HD + 2);
     __amdgpu_buffer_rsrc_t r;
     __device__ __forceinline__ Part(const AttendWs& ws, int32_t wg, bool opens) {
         float* p = ws.parts + (2 * static_cast<int64_t>(wg) + (opens ? 1 : 0)) * kFloats;
@@ -550,7 +614,7 @@ __device__ __forceinline__ float weight_of(float m, float top) {
 }
 
 // Joins the parts of a unit, kLoads of them in flight at a time.
-template <int M, int HD, int kLoads>
+template <int M, int HD, int SLOT, int kLoads>
 __device__ __forceinline__ void join_rows(const AttendIn& in, const AttendWs& ws, const RowsOut& u,
                                           int32_t first, int32_t last, float v_scale) {
     constexpr int kVec = HD / 4;
@@ -565,7 +629,7 @@ __device__ __forceinline__ void join_rows(const AttendIn& in, const AttendWs& ws
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int32_t w = min(w0 + i, last);
-                const Part<M, HD> p(ws, w, w == first);
+                const Part<M, HD, SLOT> p(ws, w, w == first);
                 m[i] = p.get(row);
                 s[i] = p.get(M + row);
                 x[i] = p.get4(2 * M + row * HD + 4 * c);
@@ -593,7 +657,7 @@ __device__ __forceinline__ void join_rows(const AttendIn& in, const AttendWs& ws
 // After this workgroup's part has reached memory (a wait by every wave, and a
 // barrier): the last of the unit's workgroups joins the parts, in their order, and
 // writes the rows.
-template <int M, int HD>
+template <int M, int HD, int SLOT>
 __device__ void join_parts(const AttendIn& in, const AttendWs& ws, const RowsOut& u, int32_t first,
                            int32_t last, float v_scale, int* flag) {
     if (threadIdx.x == 0)
@@ -601,8 +665,8 @@ __device__ void join_parts(const AttendIn& in, const AttendWs& ws, const RowsOut
                 last - first;
     __syncthreads();
     if (!scalar(*flag)) return;
-    if (last - first < 4 || M >= kTileRows) join_rows<M, HD, 4>(in, ws, u, first, last, v_scale);
-    else join_rows<M, HD, 16>(in, ws, u, first, last, v_scale);
+    if (last - first < 4 || M >= kTileRows) join_rows<M, HD, SLOT, 4>(in, ws, u, first, last, v_scale);
+    else join_rows<M, HD, SLOT, 16>(in, ws, u, first, last, v_scale);
 }
 
 // This workgroup's range.
@@ -613,27 +677,32 @@ __device__ __forceinline__ WorkRange range_of(const AttendWs& ws) {
             scalar_load(&r->n), scalar_load(&r->len), scalar_load(&r->nth)};
 }
 
-// ---------------------------------------------------------------- tile kernel
+// ------------------------------------------------------------------ tile units
 
+// LDS of a workgroup, for units of either kind.
+struct UnitLds {
+    uint4 *a, *b;       // two steps of K and V (tiles) or of the waves' V (rows)
+    OddKeys* odd_keys;  // a tile's columns, or the waves' own
+    uint32_t* notes;
+    float *wm, *wl;     // the waves' maxima and sums
+    int *flag, *odd_unit;  // odd_unit: the last unit with values that are not finite
+};
+
+// `count` blocks from the range's on of a unit of 128 rows, whose first and last block
+// are at the places `begin` and `last`.
 template <int HD, bool E4M3>
-__global__ void __launch_bounds__(kAttendThreads, HD > 128 ? 1 : 2)
-attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
+__device__ __forceinline__ void tile_unit(const AttendIn& in, const KvCacheIn& cache, const AttendWs& ws,
+                                          const WorkRange& st, const Span& s, const Blocks& bl,
+                                          int64_t begin, int64_t last, int32_t count, int unit, const UnitLds& lds) {
     constexpr int RB = HD * (E4M3 ? 1 : 2);      // bytes of a cached row
     constexpr int kTile = kBlockKeys * RB / 16;  // pieces of a block
     constexpr int kCopies = kGroupKeys * RB / 1024;
     constexpr int kSteps = HD / 16, kCols = HD / 32;
-    __shared__ uint4 kA[kTile], kB[kTile], vA[kTile], vB[kTile];
-    __shared__ OddKeys odd_keys[HD];
-    __shared__ OddNotes<kTileRows, HD> notes;
-    __shared__ int flag, odd_unit;  // the last of this workgroup's units with values that are not finite
-    WorkRange st = range_of(ws);
-    if (st.at >= st.end) return;
+    uint4 *const kA = lds.a, *const vA = lds.a + kTile, *const kB = lds.b, *const vB = lds.b + kTile;
+    auto& notes = *reinterpret_cast<OddNotes<kTileRows, HD>*>(lds.notes);
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, n32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const HeadGroup group = in.group;
-    int unit = 0;
-    if (tid == 0) odd_unit = -1;
-    __syncthreads();
 
     // this lane's sources within a group of 16 rows, and its reads of a block
     int32_t src_k[kCopies], src_v[kCopies];
@@ -649,301 +718,283 @@ attend_tile_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
     const int v_row = E4M3 ? 8 * (i16 >> 3) + 4 * half + ((i16 >> 1) & 3) : 4 * half + (i16 >> 2);
     const int v_piece = E4M3 ? side : 2 * side + ((i16 & 3) >> 1);
     const int v_off = v_row * RB + ((v_piece ^ swz_v_tile<RB, E4M3>(v_row)) * 16) + 8 * (i16 & 1);
-
-    for (Span s{st.lo, st.n, st.len}; st.at < st.end; s = scalar_span(in, cache, st.req)) {
-        const int32_t tiles = tiles_of(s.n, group, kTileRows);
-        const Blocks bl = blocks_of(s, st.tile, group, kTileRows, in.window);
-        const int32_t count =
-            static_cast<int32_t>(min(static_cast<int64_t>(bl.count - st.block), st.end - (st.at + kTileExtra + st.block)));
-        const RowsOut u{s.lo, s.n * group.n, st.tile * kTileRows, st.head, group};
-        const float c2 = in.scale * (E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f) * kLog2e;
-        const float v_scale = E4M3 ? scalar_load(cache.v_scale + st.head) : 1.0f;
-        // this lane's row, and the tokens of the wave's rows
-        const int32_t row = u.row0 + wave * 32 + n32;
-        const bool row_ok = row < u.n_rows;
-        const int32_t tok = group.div(min(row, u.n_rows - 1));
-        const int32_t base = s.len - s.n;
-        const int32_t pos = base + tok;  // (rows past the last repeat it and are not stored)
-        const int32_t wrow0 = u.row0 + wave * 32;
-        const bool wave_on = wrow0 < u.n_rows;
-        const int32_t p_first = base + group.div(min(wrow0, u.n_rows - 1));
-        const int32_t p_last = base + group.div(min(wrow0 + 31, u.n_rows - 1));
-        bf16x8_t Q[kSteps];
-        {
-            const uint16_t* qr = in.q + (u.lo + tok) * in.q_stride +
-                                 static_cast<int64_t>(u.head * group.n + min(row, u.n_rows - 1) - tok * group.n) * HD;
+    const RowsOut u{s.lo, s.n * group.n, st.tile * kTileRows, st.head, group};
+    const float c2 = in.scale * (E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f) * kLog2e;
+    const float v_scale = E4M3 ? scalar_load(cache.v_scale + st.head) : 1.0f;
+    // this lane's row, and the tokens of the wave's rows
+    const int32_t row = u.row0 + wave * 32 + n32;
+    const bool row_ok = row < u.n_rows;
+    const int32_t tok = group.div(min(row, u.n_rows - 1));
+    const int32_t base = s.len - s.n;
+    const int32_t pos = base + tok;  // (rows past the last repeat it and are not stored)
+    const int32_t wrow0 = u.row0 + wave * 32;
+    const bool wave_on = wrow0 < u.n_rows;
+    const int32_t p_first = base + group.div(min(wrow0, u.n_rows - 1));
+    const int32_t p_last = base + group.div(min(wrow0 + 31, u.n_rows - 1));
+    bf16x8_t Q[kSteps];
+    {
+        const uint16_t* qr = in.q + (u.lo + tok) * in.q_stride +
+                             static_cast<int64_t>(u.head * group.n + min(row, u.n_rows - 1) - tok * group.n) * HD;
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                const int c = E4M3 ? 4 * (i >> 1) + 2 * half + (i & 1) : 2 * i + half;
-                Q[i] = as_bf16x8(reinterpret_cast<const uint4*>(qr)[c]);
+        for (int i = 0; i < kSteps; ++i) {
+            const int c = E4M3 ? 4 * (i >> 1) + 2 * half + (i & 1) : 2 * i + half;
+            Q[i] = as_bf16x8(reinterpret_cast<const uint4*>(qr)[c]);
+        }
+    }
+
+    constexpr int kGroups = kBlockKeys / kGroupKeys;
+    int32_t ids;        // of the block to be copied next
+    uint32_t gone = 0;  // of the block whose turn it is
+    auto load_ids = [&](int32_t block) __attribute__((always_inline)) {
+        ids = page_ids(cache, st.req, block * kBlockKeys, s.len, kGroups);
+    };
+    // Copies a block and asks for the ids of the one after it.
+    auto stage = [&](int32_t block, uint4* kd, uint4* vd) __attribute__((always_inline)) {
+        const int32_t key = block * kBlockKeys + wave * kGroupKeys;
+        const int32_t page = __builtin_amdgcn_readlane(ids, wave);
+        const uint32_t next_gone = groups_gone(cache, ids, kGroups);
+        const __amdgpu_buffer_rsrc_t kr = group_rows<RB>(cache.k, cache, page, st.head, key, s.len);
+        const __amdgpu_buffer_rsrc_t vr = group_rows<RB>(cache.v, cache, page, st.head, key, s.len);
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i)
+            copy16(kr, kd + wave * (kTile / 4) + i * 64, src_k[i]);
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i)
+            copy16(vr, vd + wave * (kTile / 4) + i * 64, src_v[i]);
+        load_ids(block + 1);
+        return next_gone;
+    };
+
+    float m, l;
+    f32x16_t O[kCols];
+    bool careful = false;
+    // One block: scores, weights, O.
+    auto block_step = [&](int32_t block, const uint4* kt, uint4* vt) __attribute__((always_inline)) {
+        const int32_t key0 = block * kBlockKeys;
+        if (careful) {
+            for (int c = tid; c < HD; c += kAttendThreads) lds.odd_keys[c] = OddKeys{0, 0};
+            __syncthreads();
+            for (int e = tid; e < kTile; e += kAttendThreads) {
+                const int kr = e / (RB / 16), slot = (e % (RB / 16)) ^ swz_v_tile<RB, E4M3>(kr);
+                take_odd<E4M3>(vt + e, lds.odd_keys + slot * (E4M3 ? 16 : 8), kr);
+            }
+            __syncthreads();
+            const int r = tid % kTileRows;
+            notes.note(tid / kTileRows, r,
+                       seen_keys(key0, base + group.div(min(u.row0 + r, u.n_rows - 1)), in.window, gone),
+                       lds.odd_keys);
+        }
+        if (!wave_on || key0 > p_last) return;
+        f32x16_t S[2] = {f32x16_t{}, f32x16_t{}};
+        {
+            constexpr int kReads = E4M3 ? kSteps : 2 * kSteps;  // a step of both halves of the keys
+            const int ko = fresh(k_off);
+            auto read_k = [&](int i) { return *at_bytes(kt + 32 * (i & 1) * (RB / 16), ko ^ (32 * (i >> 1))); };
+            uint4 w[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) w[i] = read_k(i);
+            keep_order();
+#pragma unroll
+            for (int i = 0; i < kReads; ++i) {
+                const int b = i & 1, step = i >> 1;
+                const uint4 x = w[i % kAhead];
+                if constexpr (E4M3) {
+                    S[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e4m3_to_bf16(x.x, x.y), Q[2 * step], S[b], 0, 0, 0);
+                    S[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e4m3_to_bf16(x.z, x.w), Q[2 * step + 1], S[b], 0, 0, 0);
+                } else {
+                    S[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x), Q[step], S[b], 0, 0, 0);
+                }
+                if (i + kAhead < kReads) w[i % kAhead] = read_k(i + kAhead);
+                keep_order();
             }
         }
-
-        constexpr int kGroups = kBlockKeys / kGroupKeys;
-        int32_t ids;        // of the block to be copied next
-        uint32_t gone = 0;  // of the block whose turn it is
-        auto load_ids = [&](int32_t block) __attribute__((always_inline)) {
-            ids = page_ids(cache, st.req, block * kBlockKeys, s.len, kGroups);
-        };
-        // Copies a block and asks for the ids of the one after it.
-        auto stage = [&](int32_t block, uint4* kd, uint4* vd) __attribute__((always_inline)) {
-            const int32_t key = block * kBlockKeys + wave * kGroupKeys;
-            const int32_t page = __builtin_amdgcn_readlane(ids, wave);
-            const uint32_t next_gone = groups_gone(cache, ids, kGroups);
-            const __amdgpu_buffer_rsrc_t kr = group_rows<RB>(cache.k, cache, page, st.head, key, s.len);
-            const __amdgpu_buffer_rsrc_t vr = group_rows<RB>(cache.v, cache, page, st.head, key, s.len);
-#pragma unroll
-            for (int i = 0; i < kCopies; ++i)
-                copy16(kr, kd + wave * (kTile / 4) + i * 64, src_k[i]);
-#pragma unroll
-            for (int i = 0; i < kCopies; ++i)
-                copy16(vr, vd + wave * (kTile / 4) + i * 64, src_v[i]);
-            load_ids(block + 1);
-            return next_gone;
-        };
-
-        float m, l;
-        f32x16_t O[kCols];
-        bool careful = false;
-        // One block: scores, weights, O.
-        auto block_step = [&](int32_t block, const uint4* kt, uint4* vt) __attribute__((always_inline)) {
-            const int32_t key0 = block * kBlockKeys;
-            if (careful) {
-                for (int c = tid; c < HD; c += kAttendThreads) odd_keys[c] = OddKeys{0, 0};
-                __syncthreads();
-                for (int e = tid; e < kTile; e += kAttendThreads) {
-                    const int kr = e / (RB / 16), slot = (e % (RB / 16)) ^ swz_v_tile<RB, E4M3>(kr);
-                    take_odd<E4M3>(vt + e, odd_keys + slot * (E4M3 ? 16 : 8), kr);
-                }
-                __syncthreads();
-                const int r = tid % kTileRows;
-                notes.note(tid / kTileRows, r,
-                           seen_keys(key0, base + group.div(min(u.row0 + r, u.n_rows - 1)), in.window, gone),
-                           odd_keys);
-            }
-            if (!wave_on || key0 > p_last) return;
-            f32x16_t S[2] = {f32x16_t{}, f32x16_t{}};
-            {
-                constexpr int kReads = E4M3 ? kSteps : 2 * kSteps;  // a step of both halves of the keys
-                const int ko = fresh(k_off);
-                auto read_k = [&](int i) { return *at_bytes(kt + 32 * (i & 1) * (RB / 16), ko ^ (32 * (i >> 1))); };
-                uint4 w[kAhead];
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) w[i] = read_k(i);
-                keep_order();
-#pragma unroll
-                for (int i = 0; i < kReads; ++i) {
-                    const int b = i & 1, step = i >> 1;
-                    const uint4 x = w[i % kAhead];
-                    if constexpr (E4M3) {
-                        S[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e4m3_to_bf16(x.x, x.y), Q[2 * step], S[b], 0, 0, 0);
-                        S[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e4m3_to_bf16(x.z, x.w), Q[2 * step + 1], S[b], 0, 0, 0);
-                    } else {
-                        S[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x), Q[step], S[b], 0, 0, 0);
-                    }
-                    if (i + kAhead < kReads) w[i % kAhead] = read_k(i + kAhead);
-                    keep_order();
-                }
-            }
-            if (gone || key0 + kBlockKeys - 1 > p_first ||
-                (in.window > 0 && key0 <= p_last - in.window)) {
-                if (gone && lane == 0 && key0 < s.len) atomicOr(in.err_word, kErrKvPage);
-                const int32_t from = in.window > 0 ? pos - in.window : -1;
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int k = 32 * b + 8 * (i / 4) + 4 * half + i % 4;
-                        const bool see = key0 + k <= pos && key0 + k > from && !((gone >> (k / kGroupKeys)) & 1u);
-                        if (!see) S[b][i] = -INFINITY;
-                    }
-            }
-            float top = S[0][0];
-#pragma unroll
-            for (int i = 1; i < 32; ++i) top = fmaxf(top, S[i / 16][i % 16]);
-            top = half_max(top) * c2;
-            const bool raise = top > m + kRaise;
-            if (__any(raise)) {
-                const float m2 = raise ? top : m;
-                const float fade = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - m2);
-                m = m2;
-                l *= fade;
-#pragma unroll
-                for (int h = 0; h < kCols; ++h)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) O[h][i] *= fade;
-            }
-            const float off = m == -INFINITY ? 0.0f : m;
-            // V^T operand j: column block j % kCols, 16 keys at j / kCols
-            const int vo = fresh(v_off);
-            auto read_v = [&](int j) {
-                const int t = j / kCols, h = j % kCols;
-                uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                if constexpr (E4M3) {
-                    const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                        (lds_i32x2)at_bytes(vt, (vo ^ (32 * h)) + 16 * t * RB)));
-                    w.x = x.x;
-                    w.y = x.y;
-                } else {
-                    const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds_s16x4)at_bytes(vt, (vo ^ (64 * h)) + 16 * t * RB)));
-                    const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds_s16x4)at_bytes(vt, (vo ^ (64 * h)) + (16 * t + 8) * RB)));
-                    w = make_uint4(x.x, x.y, y.x, y.y);
-                }
-                return w;
-            };
-            uint4 vw[kAhead];
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) vw[j] = read_v(j);
-            keep_order();
-            uint32_t P[2][8];
-            float sum = 0.0f;
+        if (gone || key0 + kBlockKeys - 1 > p_first ||
+            (in.window > 0 && key0 <= p_last - in.window)) {
+            if (gone && lane == 0 && key0 < s.len) atomicOr(in.err_word, kErrKvPage);
+            const int32_t from = in.window > 0 ? pos - in.window : -1;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(S[b][i], c2, -off));
-                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(S[b][i + 1], c2, -off));
-                    sum += x;
-                    sum += y;
-                    P[b][i / 2] = weights2(x, y);
+                for (int i = 0; i < 16; ++i) {
+                    const int k = 32 * b + 8 * (i / 4) + 4 * half + i % 4;
+                    const bool see = key0 + k <= pos && key0 + k > from && !((gone >> (k / kGroupKeys)) & 1u);
+                    if (!see) S[b][i] = -INFINITY;
                 }
-            l += sum;
+        }
+        float top = S[0][0];
 #pragma unroll
-            for (int j = 0; j < 4 * kCols; ++j) {
-                const int t = j / kCols, h = j % kCols, b = t / 2, i0 = 4 * (t % 2);
-                const bf16x8_t p = as_bf16x8(make_uint4(P[b][i0], P[b][i0 + 1], P[b][i0 + 2], P[b][i0 + 3]));
-                bf16x8_t v;
-                if constexpr (E4M3) v = e4m3_to_bf16(vw[j % kAhead].x, vw[j % kAhead].y);
-                else v = as_bf16x8(vw[j % kAhead]);
-                O[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p, O[h], 0, 0, 0);
-                if (j + kAhead < 4 * kCols) vw[j % kAhead] = read_v(j + kAhead);
-                keep_order();
-            }
-        };
-        for (;;) {
-            m = -INFINITY;
-            l = 0.0f;
-#pragma unroll
-            for (int h = 0; h < kCols; ++h) O[h] = f32x16_t{};
-            const int32_t b0 = bl.first + st.block;
-            if (careful) {
-                notes.clear(tid);
-                __syncthreads();
-            }
-            load_ids(b0);
-            gone = stage(b0, kA, vA);
-            for (int32_t i = 0; i < count; i += 2) {
-                uint32_t after = 0;
-                __builtin_amdgcn_s_waitcnt(0);
-                __syncthreads();
-                if (i + 1 < count) after = stage(b0 + i + 1, kB, vB);
-                block_step(b0 + i, kA, vA);
-                gone = after;
-                if (i + 1 >= count) break;
-                __builtin_amdgcn_s_waitcnt(0);
-                __syncthreads();
-                if (i + 2 < count) after = stage(b0 + i + 2, kA, vA);
-                block_step(b0 + i + 1, kB, vB);
-                gone = after;
-            }
-            // any value of O that is not finite makes this NaN
-            float odd = 0.0f;
+        for (int i = 1; i < 32; ++i) top = fmaxf(top, S[i / 16][i % 16]);
+        top = half_max(top) * c2;
+        const bool raise = top > m + kRaise;
+        if (__any(raise)) {
+            const float m2 = raise ? top : m;
+            const float fade = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - m2);
+            m = m2;
+            l *= fade;
 #pragma unroll
             for (int h = 0; h < kCols; ++h)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) odd = __builtin_fmaf(O[h][i], 0.0f, odd);
-            if (__any(odd != odd) && lane == 0) odd_unit = unit;
-            l = half_sum(l);
-            if (careful) {
-                __syncthreads();
-#pragma unroll
-                for (int h = 0; h < kCols; ++h)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        O[h][i] = notes.apply(O[h][i], wave * 32 + n32, 32 * h + 8 * (i / 4) + 4 * half + i % 4);
-            }
-            if (count == bl.count) {
-                if (row_ok) {
-                    const float inv = l == 0.0f ? 0.0f : v_scale / l;
-                    uint16_t* out = out_row(in, u, wave * 32 + n32, HD);
-#pragma unroll
-                    for (int h = 0; h < kCols; ++h)
-#pragma unroll
-                        for (int i = 0; i < 16; i += 4)
-                            *reinterpret_cast<uint2*>(out + 32 * h + 2 * i + 4 * half) =
-                                make_uint2(weights2(O[h][i] * inv, O[h][i + 1] * inv),
-                                           weights2(O[h][i + 2] * inv, O[h][i + 3] * inv));
-                    if (half == 0) store_lse(in, u, wave * 32 + n32, m, l);
-                }
+                for (int i = 0; i < 16; ++i) O[h][i] *= fade;
+        }
+        const float off = m == -INFINITY ? 0.0f : m;
+        // V^T operand j: column block j % kCols, 16 keys at j / kCols
+        const int vo = fresh(v_off);
+        auto read_v = [&](int j) {
+            const int t = j / kCols, h = j % kCols;
+            uint4 w = make_uint4(0u, 0u, 0u, 0u);
+            if constexpr (E4M3) {
+                const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                    (lds_i32x2)at_bytes(vt, (vo ^ (32 * h)) + 16 * t * RB)));
+                w.x = x.x;
+                w.y = x.y;
             } else {
-                const Part<kTileRows, HD> part(ws, st.nth, st.block == 0);
-                const int r = wave * 32 + n32;
-                if (half == 0) {
-                    part.put(r, m);
-                    part.put(kTileRows + r, l);
-                }
+                const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_s16x4)at_bytes(vt, (vo ^ (64 * h)) + 16 * t * RB)));
+                const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_s16x4)at_bytes(vt, (vo ^ (64 * h)) + (16 * t + 8) * RB)));
+                w = make_uint4(x.x, x.y, y.x, y.y);
+            }
+            return w;
+        };
+        uint4 vw[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) vw[j] = read_v(j);
+        keep_order();
+        uint32_t P[2][8];
+        float sum = 0.0f;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(S[b][i], c2, -off));
+                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(S[b][i + 1], c2, -off));
+                sum += x;
+                sum += y;
+                P[b][i / 2] = weights2(x, y);
+            }
+        l += sum;
+#pragma unroll
+        for (int j = 0; j < 4 * kCols; ++j) {
+            const int t = j / kCols, h = j % kCols, b = t / 2, i0 = 4 * (t % 2);
+            const bf16x8_t p = as_bf16x8(make_uint4(P[b][i0], P[b][i0 + 1], P[b][i0 + 2], P[b][i0 + 3]));
+            bf16x8_t v;
+            if constexpr (E4M3) v = e4m3_to_bf16(vw[j % kAhead].x, vw[j % kAhead].y);
+            else v = as_bf16x8(vw[j % kAhead]);
+            O[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p, O[h], 0, 0, 0);
+            if (j + kAhead < 4 * kCols) vw[j % kAhead] = read_v(j + kAhead);
+            keep_order();
+        }
+    };
+    for (;;) {
+        m = -INFINITY;
+        l = 0.0f;
+#pragma unroll
+        for (int h = 0; h < kCols; ++h) O[h] = f32x16_t{};
+        const int32_t b0 = bl.first + st.block;
+        if (careful) {
+            notes.clear(tid);
+            __syncthreads();
+        }
+        load_ids(b0);
+        gone = stage(b0, kA, vA);
+        for (int32_t i = 0; i < count; i += 2) {
+            uint32_t after = 0;
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+            if (i + 1 < count) after = stage(b0 + i + 1, kB, vB);
+            block_step(b0 + i, kA, vA);
+            gone = after;
+            if (i + 1 >= count) break;
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+            if (i + 2 < count) after = stage(b0 + i + 2, kA, vA);
+            block_step(b0 + i + 1, kB, vB);
+            gone = after;
+        }
+        // any value of O that is not finite makes this NaN
+        float odd = 0.0f;
+#pragma unroll
+        for (int h = 0; h < kCols; ++h)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) odd = __builtin_fmaf(O[h][i], 0.0f, odd);
+        if (__any(odd != odd) && lane == 0) *lds.odd_unit = unit;
+        l = half_sum(l);
+        if (careful) {
+            __syncthreads();
+#pragma unroll
+            for (int h = 0; h < kCols; ++h)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    O[h][i] = notes.apply(O[h][i], wave * 32 + n32, 32 * h + 8 * (i / 4) + 4 * half + i % 4);
+        }
+        if (count == bl.count) {
+            if (row_ok) {
+                const float inv = l == 0.0f ? 0.0f : v_scale / l;
+                uint16_t* out = out_row(in, u, wave * 32 + n32, HD);
 #pragma unroll
                 for (int h = 0; h < kCols; ++h)
 #pragma unroll
                     for (int i = 0; i < 16; i += 4)
-                        part.put4(2 * kTileRows + r * HD + 32 * h + 2 * i + 4 * half,
-                                  f32x4_t{O[h][i], O[h][i + 1], O[h][i + 2], O[h][i + 3]});
-                __builtin_amdgcn_s_waitcnt(0);
+                        *reinterpret_cast<uint2*>(out + 32 * h + 2 * i + 4 * half) =
+                            make_uint2(weights2(O[h][i] * inv, O[h][i + 1] * inv),
+                                       weights2(O[h][i + 2] * inv, O[h][i + 3] * inv));
+                if (half == 0) store_lse(in, u, wave * 32 + n32, m, l);
             }
-            __syncthreads();  // the buffers are free, a part has reached memory, odd_unit is known
-            if (careful || scalar(odd_unit) != unit) break;
-            careful = true;
-        }
-        if (count != bl.count) {
-            const int64_t begin = st.at + kTileExtra;
-            join_parts<kTileRows, HD>(in, ws, u, static_cast<int32_t>(begin / st.share),
-                                      static_cast<int32_t>((begin + bl.count - 1) / st.share), v_scale, &flag);
-        }
-        ++unit;
-
-        if (st.block + count < bl.count) break;
-        st.at += kTileExtra + bl.count;
-        st.block = 0;
-        if (++st.tile == tiles) {
-            st.tile = 0;
-            if (++st.head == cache.n_kv) {
-                st.head = 0;
-                if (st.at < st.end)
-                    do ++st.req;
-                    while (st.req < cache.R_max - 1 && scalar_span(in, cache, st.req).n == 0);
+        } else {
+            const Part<kTileRows, HD, kTileRows> part(ws, st.nth, st.block == 0);
+            const int r = wave * 32 + n32;
+            if (half == 0) {
+                part.put(r, m);
+                part.put(kTileRows + r, l);
             }
+#pragma unroll
+            for (int h = 0; h < kCols; ++h)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    part.put4(2 * kTileRows + r * HD + 32 * h + 2 * i + 4 * half,
+                              f32x4_t{O[h][i], O[h][i + 1], O[h][i + 2], O[h][i + 3]});
+            __builtin_amdgcn_s_waitcnt(0);
         }
+        __syncthreads();  // the buffers are free, a part has reached memory, odd_unit is known
+        if (careful || scalar(*lds.odd_unit) != unit) break;
+        careful = true;
+    }
+    if (count != bl.count) {
+        join_parts<kTileRows, HD, kTileRows>(in, ws, u, static_cast<int32_t>(begin / st.share),
+                                  static_cast<int32_t>(last / st.share), v_scale, lds.flag);
     }
 }
 
-// ----------------------------------------------------------------- row kernel
+// ------------------------------------------------------------------- row units
 
-template <int HD, bool E4M3, int NB>
-__global__ void __launch_bounds__(kAttendThreads, HD > 128 ? 1 : 2)
-attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
+// Pieces of V that a wave copies for a step of row units, and the step's keys.
+template <int HD, bool E4M3>
+struct RowStep {
+    static constexpr int kKeys = !E4M3 && HD >= 128 ? 32 : 64;
+    static constexpr int kTile = kKeys * HD * (E4M3 ? 1 : 2) / 16;
+};
+
+// The same of a unit of 16 NB rows; SLOT: rows that a part has room for.
+template <int HD, bool E4M3, int NB, int SLOT>
+__device__ __forceinline__ void row_unit(const AttendIn& in, const KvCacheIn& cache, const AttendWs& ws,
+                                         const WorkRange& st, const Span& s, const Blocks& bl,
+                                         int64_t begin, int64_t last, int32_t count, int unit, const UnitLds& lds) {
     constexpr int RB = HD * (E4M3 ? 1 : 2);
-    constexpr int KS = !E4M3 && RB >= 256 ? 32 : 64;  // keys of a step: 8 KB of V, or more
+    constexpr int KS = RowStep<HD, E4M3>::kKeys;
     constexpr int kGroups = KS / kGroupKeys;
     constexpr int kLoads = RB / 64;               // 16-byte loads of a lane per 16 keys
     constexpr int kCopies = kGroupKeys * RB / 1024;
     constexpr int kSteps = HD / 32, kCols = HD / 16, M = 16 * NB;
     constexpr int kTile = KS * RB / 16;           // pieces of a step's V
     static_assert(kAttendWaves * kTile >= kAttendWaves * 16 * HD / 4, "room to join the waves");
-    __shared__ uint4 vA[kAttendWaves * kTile], vB[kAttendWaves * kTile];
-    __shared__ float wm[kAttendWaves][M], wl[kAttendWaves][M];
-    __shared__ OddKeys odd_keys[kAttendWaves][HD];
-    __shared__ OddNotes<M, HD> notes;
-    __shared__ int flag, odd_unit;  // the last of this workgroup's units with values that are not finite
-    WorkRange st = range_of(ws);
-    if (st.at >= st.end) return;
+    uint4 *const vA = lds.a, *const vB = lds.b;
+    auto* const wm = reinterpret_cast<float (*)[M]>(lds.wm);
+    auto* const wl = reinterpret_cast<float (*)[M]>(lds.wl);
+    auto* const odd_keys = reinterpret_cast<OddKeys (*)[HD]>(lds.odd_keys);
+    auto& notes = *reinterpret_cast<OddNotes<M, HD>*>(lds.notes);
     const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, n16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const HeadGroup group = in.group;
-    int unit = 0;
-    if (tid == 0) odd_unit = -1;
-    __syncthreads();
 
     // This lane's K, its part of V's copies and its reads of V.  A copy of 1 KB takes
     // 1024 / RB rows, so the permutation, by the row's low bits, changes from copy
@@ -960,298 +1011,332 @@ attend_row_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
     const int v_piece = E4M3 ? 0 : (n16 & 3) >> 1;
     const int v_off = wave * kTile * 16 + v_row * RB + ((v_piece ^ swz_v_row<RB, E4M3>(v_row)) * 16) +
                       8 * (n16 & 1);
+    const RowsOut u{s.lo, s.n * group.n, 0, st.head, group};
+    const float c2 = in.scale * (E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f) * kLog2e;
+    const int32_t base = s.len - s.n;
+    const int32_t p_first = base, p_last = s.len - 1;
+    int32_t pos[NB];
+    bf16x8_t Q[NB][kSteps];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int32_t row = 16 * b + n16, held = min(row, u.n_rows - 1), tok = group.div(held);
+        pos[b] = base + tok;  // (rows past the last repeat it and are not stored)
+        const uint16_t* qr = in.q + (u.lo + tok) * in.q_stride +
+                             static_cast<int64_t>(u.head * group.n + held - tok * group.n) * HD;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            const int c = E4M3 ? 8 * (i >> 1) + 2 * g4 + (i & 1) : 4 * i + g4;
+            Q[b][i] = as_bf16x8(reinterpret_cast<const uint4*>(qr)[c]);
+        }
+    }
+    // this wave's steps: of the segment's, every fourth
+    const int32_t key_from = (bl.first + st.block) * kBlockKeys;
+    const int32_t steps = count * (kBlockKeys / KS);
 
-    for (Span s{st.lo, st.n, st.len}; st.at < st.end; s = scalar_span(in, cache, st.req)) {
-        const Blocks bl = blocks_of(s, 0, group, M, in.window);
-        const int32_t count =
-            static_cast<int32_t>(min(static_cast<int64_t>(bl.count - st.block), st.end - (st.at + kRowExtra + st.block)));
-        const RowsOut u{s.lo, s.n * group.n, 0, st.head, group};
-        const float c2 = in.scale * (E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f) * kLog2e;
-        const int32_t base = s.len - s.n;
-        const int32_t p_first = base, p_last = s.len - 1;
-        int32_t pos[NB];
-        bf16x8_t Q[NB][kSteps];
+    uint4 KA[kGroups][kLoads], KB[kGroups][kLoads];
+    uint32_t goneA, goneB;
+    // Every step of the pipeline issues its loads, past the last one of nothing
+    // (resources without rows): with a branch around them the wait for one step's
+    // K would be for everything outstanding.
+    int32_t ids;  // page ids of the step whose loads come next
+    auto load_ids = [&](int32_t step) __attribute__((always_inline)) {
+        ids = page_ids(cache, st.req, key_from + step * KS, s.len, kGroups);
+    };
+    auto stage = [&](int32_t step, uint4 (&K)[kGroups][kLoads], uint4* vd, uint32_t& gone)
+        __attribute__((always_inline)) {
+        const int32_t key0 = key_from + step * KS, len = step < steps ? s.len : 0;
+        __amdgpu_buffer_rsrc_t vr[kGroups];
+        int32_t page[kGroups];
+        gone = groups_gone(cache, ids, kGroups);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int32_t row = 16 * b + n16, held = min(row, u.n_rows - 1), tok = group.div(held);
-            pos[b] = base + tok;  // (rows past the last repeat it and are not stored)
-            const uint16_t* qr = in.q + (u.lo + tok) * in.q_stride +
-                                 static_cast<int64_t>(u.head * group.n + held - tok * group.n) * HD;
+        for (int g = 0; g < kGroups; ++g) page[g] = __builtin_amdgcn_readlane(ids, g);
+        load_ids(step + kAttendWaves);
+        const int ko = fresh(k_src);
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                const int c = E4M3 ? 8 * (i >> 1) + 2 * g4 + (i & 1) : 4 * i + g4;
-                Q[b][i] = as_bf16x8(reinterpret_cast<const uint4*>(qr)[c]);
+        for (int g = 0; g < kGroups; ++g) {
+            const int32_t key = key0 + g * kGroupKeys;
+            const __amdgpu_buffer_rsrc_t kr = group_rows<RB>(cache.k, cache, page[g], st.head, key, len);
+            vr[g] = group_rows<RB>(cache.v, cache, page[g], st.head, key, len);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const u32x4_t w = __builtin_bit_cast(
+                    u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(kr, ko + 64 * i, 0, kOnce));
+                K[g][i] = make_uint4(w.x, w.y, w.z, w.w);
             }
         }
-        // this wave's steps: of the segment's, every fourth
-        const int32_t key_from = (bl.first + st.block) * kBlockKeys;
-        const int32_t steps = count * (kBlockKeys / KS);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i)
+                copy16<kOnce>(vr[g], vd + wave * kTile + g * (kGroupKeys * RB / 16) + i * 64,
+                              src_v[g * kCopies + i] + 1024 * i);
+    };
 
-        uint4 KA[kGroups][kLoads], KB[kGroups][kLoads];
-        uint32_t goneA, goneB;
-        // Every step of the pipeline issues its loads, past the last one of nothing
-        // (resources without rows): with a branch around them the wait for one step's
-        // K would be for everything outstanding.
-        int32_t ids;  // page ids of the step whose loads come next
-        auto load_ids = [&](int32_t step) __attribute__((always_inline)) {
-            ids = page_ids(cache, st.req, key_from + step * KS, s.len, kGroups);
-        };
-        auto stage = [&](int32_t step, uint4 (&K)[kGroups][kLoads], uint4* vd, uint32_t& gone)
-            __attribute__((always_inline)) {
-            const int32_t key0 = key_from + step * KS, len = step < steps ? s.len : 0;
-            __amdgpu_buffer_rsrc_t vr[kGroups];
-            int32_t page[kGroups];
-            gone = groups_gone(cache, ids, kGroups);
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) page[g] = __builtin_amdgcn_readlane(ids, g);
-            load_ids(step + kAttendWaves);
-            const int ko = fresh(k_src);
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-                const int32_t key = key0 + g * kGroupKeys;
-                const __amdgpu_buffer_rsrc_t kr = group_rows<RB>(cache.k, cache, page[g], st.head, key, len);
-                vr[g] = group_rows<RB>(cache.v, cache, page[g], st.head, key, len);
-#pragma unroll
-                for (int i = 0; i < kLoads; ++i) {
-                    const u32x4_t w = __builtin_bit_cast(
-                        u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(kr, ko + 64 * i, 0, kOnce));
-                    K[g][i] = make_uint4(w.x, w.y, w.z, w.w);
-                }
+    float m[NB], l[NB];
+    f32x4_t O[NB][kCols];
+    bool careful = false;
+    auto key_step = [&](int32_t step, const uint4 (&K)[kGroups][kLoads], uint4* vt, uint32_t gone)
+        __attribute__((always_inline)) {
+        const int32_t key0 = key_from + step * KS;
+        if (careful) {  // the tile and the masks are this wave's own
+            for (int c = lane; c < HD; c += kWave) odd_keys[wave][c] = OddKeys{0, 0};
+            __builtin_amdgcn_s_waitcnt(0);
+            for (int e = lane; e < kTile; e += kWave) {
+                const int kr = e / (RB / 16), slot = (e % (RB / 16)) ^ swz_v_row<RB, E4M3>(kr);
+                take_odd<E4M3>(vt + wave * kTile + e, odd_keys[wave] + slot * (E4M3 ? 16 : 8), kr);
             }
+            __builtin_amdgcn_s_waitcnt(0);
+            if (lane < 2 * M)
+                notes.note(lane / M, lane % M,
+                           seen_keys(key0, base + group.div(min(lane % M, u.n_rows - 1)), in.window, gone),
+                           odd_keys[wave]);
+        }
+        f32x4_t S[NB][kGroups];
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g)
+        for (int g = 0; g < kGroups; ++g) {
 #pragma unroll
-                for (int i = 0; i < kCopies; ++i)
-                    copy16<kOnce>(vr[g], vd + wave * kTile + g * (kGroupKeys * RB / 16) + i * 64,
-                                  src_v[g * kCopies + i] + 1024 * i);
-        };
-
-        float m[NB], l[NB];
-        f32x4_t O[NB][kCols];
-        bool careful = false;
-        auto key_step = [&](int32_t step, const uint4 (&K)[kGroups][kLoads], uint4* vt, uint32_t gone)
-            __attribute__((always_inline)) {
-            const int32_t key0 = key_from + step * KS;
-            if (careful) {  // the tile and the masks are this wave's own
-                for (int c = lane; c < HD; c += kWave) odd_keys[wave][c] = OddKeys{0, 0};
-                __builtin_amdgcn_s_waitcnt(0);
-                for (int e = lane; e < kTile; e += kWave) {
-                    const int kr = e / (RB / 16), slot = (e % (RB / 16)) ^ swz_v_row<RB, E4M3>(kr);
-                    take_odd<E4M3>(vt + wave * kTile + e, odd_keys[wave] + slot * (E4M3 ? 16 : 8), kr);
-                }
-                __builtin_amdgcn_s_waitcnt(0);
-                if (lane < 2 * M)
-                    notes.note(lane / M, lane % M,
-                               seen_keys(key0, base + group.div(min(lane % M, u.n_rows - 1)), in.window, gone),
-                               odd_keys[wave]);
-            }
-            f32x4_t S[NB][kGroups];
+            for (int b = 0; b < NB; ++b) S[b][g] = f32x4_t{};
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-#pragma unroll
-                for (int b = 0; b < NB; ++b) S[b][g] = f32x4_t{};
-#pragma unroll
-                for (int i = 0; i < kSteps; ++i) {
-                    bf16x8_t k;
-                    if constexpr (E4M3) {
-                        const uint4 w = K[g][i >> 1];
-                        k = i & 1 ? e4m3_to_bf16(w.z, w.w) : e4m3_to_bf16(w.x, w.y);
-                    } else {
-                        k = as_bf16x8(K[g][i]);
-                    }
-#pragma unroll
-                    for (int b = 0; b < NB; ++b)
-                        S[b][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, Q[b][i], S[b][g], 0, 0, 0);
-                }
-            }
-            if (gone || key0 + KS - 1 > p_first || (in.window > 0 && key0 <= p_last - in.window)) {
-                if (gone && lane == 0 && key0 < s.len) atomicOr(in.err_word, kErrKvPage);
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    const int32_t from = in.window > 0 ? pos[b] - in.window : -1;
-#pragma unroll
-                    for (int g = 0; g < kGroups; ++g)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int32_t k = key0 + 16 * g + 4 * g4 + i;
-                            if (!(k <= pos[b] && k > from && !((gone >> g) & 1u))) S[b][g][i] = -INFINITY;
-                        }
-                }
-            }
-            float top[NB];
-            bool raise = false;
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                top[b] = S[b][0][0];
-#pragma unroll
-                for (int i = 1; i < 4 * kGroups; ++i) top[b] = fmaxf(top[b], S[b][i / 4][i % 4]);
-                top[b] = quarter_max(top[b]) * c2;
-                raise |= top[b] > m[b] + kRaise;
-            }
-            if (__any(raise)) {
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    const float m2 = top[b] > m[b] + kRaise ? top[b] : m[b];
-                    const float fade = m[b] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[b] - m2);
-                    m[b] = m2;
-                    l[b] *= fade;
-#pragma unroll
-                    for (int h = 0; h < kCols; ++h) O[b][h] *= fade;
-                }
-            }
-            // V^T operand j: column block j % kCols, 32 keys at j / kCols
-            constexpr int kReads = kCols * kGroups / 2;
-            wait_all_but<1 + kGroups * (kLoads + kCopies)>();  // the next step's loads: V is there
-            const int vo = fresh(v_off);
-            auto read_v = [&](int j) {
-                const int t = j / kCols, h = j % kCols;
-                uint4 w = make_uint4(0u, 0u, 0u, 0u);
+            for (int i = 0; i < kSteps; ++i) {
+                bf16x8_t k;
                 if constexpr (E4M3) {
-                    const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                        (lds_i32x2)at_bytes(vt, (vo ^ (16 * h)) + 32 * t * RB)));
-                    w.x = x.x;
-                    w.y = x.y;
+                    const uint4 w = K[g][i >> 1];
+                    k = i & 1 ? e4m3_to_bf16(w.z, w.w) : e4m3_to_bf16(w.x, w.y);
                 } else {
-                    const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds_s16x4)at_bytes(vt, (vo ^ (32 * h)) + 32 * t * RB)));
-                    const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds_s16x4)at_bytes(vt, (vo ^ (32 * h)) + (32 * t + 16) * RB)));
-                    w = make_uint4(x.x, x.y, y.x, y.y);
+                    k = as_bf16x8(K[g][i]);
                 }
-                return w;
-            };
-            uint4 vw[kAhead];
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j) vw[j] = read_v(j);
-            keep_order();
-            uint32_t P[NB][kGroups][2];
+                for (int b = 0; b < NB; ++b)
+                    S[b][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, Q[b][i], S[b][g], 0, 0, 0);
+            }
+        }
+        if (gone || key0 + KS - 1 > p_first || (in.window > 0 && key0 <= p_last - in.window)) {
+            if (gone && lane == 0 && key0 < s.len) atomicOr(in.err_word, kErrKvPage);
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                const float off = m[b] == -INFINITY ? 0.0f : m[b];
+                const int32_t from = in.window > 0 ? pos[b] - in.window : -1;
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(S[b][g][2 * i], c2, -off));
-                        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(S[b][g][2 * i + 1], c2, -off));
-                        l[b] += x + y;
-                        P[b][g][i] = weights2(x, y);
+                    for (int i = 0; i < 4; ++i) {
+                        const int32_t k = key0 + 16 * g + 4 * g4 + i;
+                        if (!(k <= pos[b] && k > from && !((gone >> g) & 1u))) S[b][g][i] = -INFINITY;
                     }
             }
-#pragma unroll
-            for (int j = 0; j < kReads; ++j) {
-                const int t = j / kCols, h = j % kCols;
-                bf16x8_t v;
-                if constexpr (E4M3) v = e4m3_to_bf16(vw[j % kAhead].x, vw[j % kAhead].y);
-                else v = as_bf16x8(vw[j % kAhead]);
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    const bf16x8_t p = as_bf16x8(make_uint4(P[b][2 * t][0], P[b][2 * t][1], P[b][2 * t + 1][0],
-                                                            P[b][2 * t + 1][1]));
-                    O[b][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, O[b][h], 0, 0, 0);
-                }
-                if (j + kAhead < kReads) vw[j % kAhead] = read_v(j + kAhead);
-                keep_order();
-            }
-        };
-        for (;;) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                m[b] = -INFINITY;
-                l[b] = 0.0f;
-#pragma unroll
-                for (int h = 0; h < kCols; ++h) O[b][h] = f32x4_t{};
-            }
-            if (careful) {
-                notes.clear(tid);
-                __syncthreads();
-            }
-            load_ids(wave);
-            stage(wave, KA, vA, goneA);
-            for (int32_t i = wave; i < steps; i += 2 * kAttendWaves) {
-                stage(i + kAttendWaves, KB, vB, goneB);
-                key_step(i, KA, vA, goneA);
-                stage(i + 2 * kAttendWaves, KA, vA, goneA);
-                if (i + kAttendWaves < steps) key_step(i + kAttendWaves, KB, vB, goneB);
-            }
-            float odd = 0.0f;
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int h = 0; h < kCols; ++h)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) odd = __builtin_fmaf(O[b][h][i], 0.0f, odd);
-            if (__any(odd != odd) && lane == 0) odd_unit = unit;
-            __builtin_amdgcn_s_waitcnt(0);  // also the copies of steps past the last
-            __syncthreads();
-            if (careful || scalar(odd_unit) != unit) break;
-            careful = true;
         }
-        ++unit;
-
-        // the waves' rows joined in LDS (where V was), 16 at a time
-        const bool whole = count == bl.count;
-        const float v_scale = E4M3 ? scalar_load(cache.v_scale + st.head) : 1.0f;
-        const Part<M, HD> part(ws, st.nth, st.block == 0);
-        f32x4_t* const pool = reinterpret_cast<f32x4_t*>(vA);
-        constexpr int kVec = HD / 4;
+        float top[NB];
+        bool raise = false;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            const float lsum = quarter_sum(l[b]);
-            if (g4 == 0) {
-                wm[wave][16 * b + n16] = m[b];
-                wl[wave][16 * b + n16] = lsum;
+            top[b] = S[b][0][0];
+#pragma unroll
+            for (int i = 1; i < 4 * kGroups; ++i) top[b] = fmaxf(top[b], S[b][i / 4][i % 4]);
+            top[b] = quarter_max(top[b]) * c2;
+            raise |= top[b] > m[b] + kRaise;
+        }
+        if (__any(raise)) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const float m2 = top[b] > m[b] + kRaise ? top[b] : m[b];
+                const float fade = m[b] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[b] - m2);
+                m[b] = m2;
+                l[b] *= fade;
+#pragma unroll
+                for (int h = 0; h < kCols; ++h) O[b][h] *= fade;
             }
-            __syncthreads();  // V (or the rows before) is no longer read
+        }
+        // V^T operand j: column block j % kCols, 32 keys at j / kCols
+        constexpr int kReads = kCols * kGroups / 2;
+        wait_all_but<1 + kGroups * (kLoads + kCopies)>();  // the next step's loads: V is there
+        const int vo = fresh(v_off);
+        auto read_v = [&](int j) {
+            const int t = j / kCols, h = j % kCols;
+            uint4 w = make_uint4(0u, 0u, 0u, 0u);
+            if constexpr (E4M3) {
+                const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                    (lds_i32x2)at_bytes(vt, (vo ^ (16 * h)) + 32 * t * RB)));
+                w.x = x.x;
+                w.y = x.y;
+            } else {
+                const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_s16x4)at_bytes(vt, (vo ^ (32 * h)) + 32 * t * RB)));
+                const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_s16x4)at_bytes(vt, (vo ^ (32 * h)) + (32 * t + 16) * RB)));
+                w = make_uint4(x.x, x.y, y.x, y.y);
+            }
+            return w;
+        };
+        uint4 vw[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) vw[j] = read_v(j);
+        keep_order();
+        uint32_t P[NB][kGroups][2];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const float off = m[b] == -INFINITY ? 0.0f : m[b];
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(S[b][g][2 * i], c2, -off));
+                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(S[b][g][2 * i + 1], c2, -off));
+                    l[b] += x + y;
+                    P[b][g][i] = weights2(x, y);
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < kReads; ++j) {
+            const int t = j / kCols, h = j % kCols;
+            bf16x8_t v;
+            if constexpr (E4M3) v = e4m3_to_bf16(vw[j % kAhead].x, vw[j % kAhead].y);
+            else v = as_bf16x8(vw[j % kAhead]);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const bf16x8_t p = as_bf16x8(make_uint4(P[b][2 * t][0], P[b][2 * t][1], P[b][2 * t + 1][0],
+                                                        P[b][2 * t + 1][1]));
+                O[b][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, O[b][h], 0, 0, 0);
+            }
+            if (j + kAhead < kReads) vw[j % kAhead] = read_v(j + kAhead);
+            keep_order();
+        }
+    };
+    for (;;) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            m[b] = -INFINITY;
+            l[b] = 0.0f;
+#pragma unroll
+            for (int h = 0; h < kCols; ++h) O[b][h] = f32x4_t{};
+        }
+        if (careful) {
+            notes.clear(tid);
+            __syncthreads();
+        }
+        load_ids(wave);
+        stage(wave, KA, vA, goneA);
+        for (int32_t i = wave; i < steps; i += 2 * kAttendWaves) {
+            stage(i + kAttendWaves, KB, vB, goneB);
+            key_step(i, KA, vA, goneA);
+            stage(i + 2 * kAttendWaves, KA, vA, goneA);
+            if (i + kAttendWaves < steps) key_step(i + kAttendWaves, KB, vB, goneB);
+        }
+        float odd = 0.0f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int h = 0; h < kCols; ++h)
-                pool[(wave * 16 + n16) * kVec + ((4 * h + g4) ^ n16)] = O[b][h];
-            __syncthreads();
-            for (int e = tid; e < 16 * kVec; e += kAttendThreads) {
-                const int r = e / kVec, c = e % kVec, row = 16 * b + r;
-                float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-                for (int w = 0; w < kAttendWaves; ++w) top = fmaxf(top, wm[w][row]);
-                f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+                for (int i = 0; i < 4; ++i) odd = __builtin_fmaf(O[b][h][i], 0.0f, odd);
+        if (__any(odd != odd) && lane == 0) *lds.odd_unit = unit;
+        __builtin_amdgcn_s_waitcnt(0);  // also the copies of steps past the last
+        __syncthreads();
+        if (careful || scalar(*lds.odd_unit) != unit) break;
+        careful = true;
+    }
+
+    // the waves' rows joined in LDS (where V was), 16 at a time
+    const bool whole = count == bl.count;
+    const float v_scale = E4M3 ? scalar_load(cache.v_scale + st.head) : 1.0f;
+    const Part<M, HD, SLOT> part(ws, st.nth, st.block == 0);
+    f32x4_t* const pool = reinterpret_cast<f32x4_t*>(vA);
+    constexpr int kVec = HD / 4;
 #pragma unroll
-                for (int w = 0; w < kAttendWaves; ++w) {
-                    const float f = weight_of(wm[w][row], top);
-                    sum += wl[w][row] * f;
-                    o += pool[(w * 16 + r) * kVec + (c ^ r)] * f;
+    for (int b = 0; b < NB; ++b) {
+        const float lsum = quarter_sum(l[b]);
+        if (g4 == 0) {
+            wm[wave][16 * b + n16] = m[b];
+            wl[wave][16 * b + n16] = lsum;
+        }
+        __syncthreads();  // V (or the rows before) is no longer read
+#pragma unroll
+        for (int h = 0; h < kCols; ++h)
+            pool[(wave * 16 + n16) * kVec + ((4 * h + g4) ^ n16)] = O[b][h];
+        __syncthreads();
+        for (int e = tid; e < 16 * kVec; e += kAttendThreads) {
+            const int r = e / kVec, c = e % kVec, row = 16 * b + r;
+            float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kAttendWaves; ++w) top = fmaxf(top, wm[w][row]);
+            f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < kAttendWaves; ++w) {
+                const float f = weight_of(wm[w][row], top);
+                sum += wl[w][row] * f;
+                o += pool[(w * 16 + r) * kVec + (c ^ r)] * f;
+            }
+            if (careful)
+                for (int i = 0; i < 4; ++i) o[i] = notes.apply(o[i], row, 4 * c + i);
+            if (!whole) {
+                if (c == 0) {
+                    part.put(row, top);
+                    part.put(M + row, sum);
                 }
-                if (careful)
-                    for (int i = 0; i < 4; ++i) o[i] = notes.apply(o[i], row, 4 * c + i);
-                if (!whole) {
-                    if (c == 0) {
-                        part.put(row, top);
-                        part.put(M + row, sum);
-                    }
-                    part.put4(2 * M + row * HD + 4 * c, o);
-                } else if (row < u.n_rows) {
-                    const float inv = sum == 0.0f ? 0.0f : v_scale / sum;
-                    *reinterpret_cast<uint2*>(out_row(in, u, row, HD) + 4 * c) =
-                        make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
-                    if (c == 0) store_lse(in, u, row, top, sum);
-                }
+                part.put4(2 * M + row * HD + 4 * c, o);
+            } else if (row < u.n_rows) {
+                const float inv = sum == 0.0f ? 0.0f : v_scale / sum;
+                *reinterpret_cast<uint2*>(out_row(in, u, row, HD) + 4 * c) =
+                    make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+                if (c == 0) store_lse(in, u, row, top, sum);
             }
         }
-        if (!whole) {
-            __builtin_amdgcn_s_waitcnt(0);
-            __syncthreads();
-            const int64_t begin = st.at + kRowExtra;
-            join_parts<M, HD>(in, ws, u, static_cast<int32_t>(begin / st.share),
-                              static_cast<int32_t>((begin + bl.count - 1) / st.share), v_scale, &flag);
-        }
-        __syncthreads();  // before V is copied in again
+    }
+    if (!whole) {
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        join_parts<M, HD, SLOT>(in, ws, u, static_cast<int32_t>(begin / st.share),
+                          static_cast<int32_t>(last / st.share), v_scale, lds.flag);
+    }
+    __syncthreads();  // before V is copied in again
+}
 
+// ----------------------------------------------------------------- the kernel
+
+// NB 0: units of 128 rows, and those of a request with few rows as row units of 16;
+// otherwise row units of 16 NB rows.
+template <int HD, bool E4M3, int NB>
+__global__ void __launch_bounds__(kAttendThreads, HD > 128 ? 1 : 2)
+attend_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
+    constexpr int RB = HD * (E4M3 ? 1 : 2);
+    constexpr int kRows = NB ? 16 * NB : kTileRows;
+    constexpr Deal kDeal = deal_of(kRows);
+    constexpr int kRowBuf = kAttendWaves * RowStep<HD, E4M3>::kTile, kTileBuf = 2 * kBlockKeys * RB / 16;
+    constexpr int kBuf = NB || kRowBuf > kTileBuf ? kRowBuf : kTileBuf;
+    __shared__ uint4 a[kBuf], b[kBuf];
+    __shared__ OddKeys odd_keys[kAttendWaves * HD];
+    __shared__ uint32_t notes[2 * kRows * HD / 32];
+    __shared__ float wm[kAttendWaves * (NB ? kRows : kFewRows)], wl[kAttendWaves * (NB ? kRows : kFewRows)];
+    __shared__ int flag, odd_unit;
+    const UnitLds lds{a, b, odd_keys, notes, wm, wl, &flag, &odd_unit};
+    WorkRange st = range_of(ws);
+    if (st.at >= st.end) return;
+    if (threadIdx.x == 0) odd_unit = -1;
+    __syncthreads();
+    int unit = 0;
+    for (Span s{st.lo, st.n, st.len}; st.at < st.end; s = scalar_span(in, cache, st.req)) {
+        const Blocks bl = blocks_of(s, st.tile, in.group, kRows, in.window);
+        const int64_t begin = st.at + kDeal.extra;
+        const int32_t step = few_rows(s.n, in.group) ? kDeal.few_step : kDeal.step, all = bl.count * step;
+        const int32_t count = static_cast<int32_t>(min(st.end - begin, static_cast<int64_t>(all))) / step - st.block;
+        if constexpr (NB) {
+            row_unit<HD, E4M3, NB, kRows>(in, cache, ws, st, s, bl, begin, begin + all - step, count, unit, lds);
+        } else {
+            if (few_rows(s.n, in.group))
+                row_unit<HD, E4M3, 1, kTileRows>(in, cache, ws, st, s, bl, begin, begin + all - step, count, unit, lds);
+            else
+                tile_unit<HD, E4M3>(in, cache, ws, st, s, bl, begin, begin + all - step, count, unit, lds);
+        }
+        ++unit;
         if (st.block + count < bl.count) break;
-        st.at += kRowExtra + bl.count;
+        st.at += kDeal.extra + all;
         st.block = 0;
-        if (++st.head == cache.n_kv) {
-            st.head = 0;
-            if (st.at < st.end)
-                do ++st.req;
-                while (st.req < cache.R_max - 1 && scalar_span(in, cache, st.req).n == 0);
+        if (NB || ++st.tile == tiles_of(s.n, in.group, kRows)) {
+            st.tile = 0;
+            if (++st.head == cache.n_kv) {
+                st.head = 0;
+                if (st.at < st.end)
+                    do ++st.req;
+                    while (st.req < cache.R_max - 1 && scalar_span(in, cache, st.req).n == 0);
+            }
         }
     }
 }
@@ -1286,12 +1371,12 @@ WsLayout ws_layout(int32_t rows, const KvCacheIn& c) {
 using AttendKernel = void (*)(AttendIn, KvCacheIn, AttendWs);
 // Indexed by head_dim (64, 128, 256), type and form (16 rows, 32 rows, tiles).
 constexpr AttendKernel kKernels[3][2][3] = {
-    {{attend_row_kernel<64, false, 1>, attend_row_kernel<64, false, 2>, attend_tile_kernel<64, false>},
-     {attend_row_kernel<64, true, 1>, attend_row_kernel<64, true, 2>, attend_tile_kernel<64, true>}},
-    {{attend_row_kernel<128, false, 1>, attend_row_kernel<128, false, 2>, attend_tile_kernel<128, false>},
-     {attend_row_kernel<128, true, 1>, attend_row_kernel<128, true, 2>, attend_tile_kernel<128, true>}},
-    {{attend_row_kernel<256, false, 1>, attend_row_kernel<256, false, 2>, attend_tile_kernel<256, false>},
-     {attend_row_kernel<256, true, 1>, attend_row_kernel<256, true, 2>, attend_tile_kernel<256, true>}}};
+    {{attend_kernel<64, false, 1>, attend_kernel<64, false, 2>, attend_kernel<64, false, 0>},
+     {attend_kernel<64, true, 1>, attend_kernel<64, true, 2>, attend_kernel<64, true, 0>}},
+    {{attend_kernel<128, false, 1>, attend_kernel<128, false, 2>, attend_kernel<128, false, 0>},
+     {attend_kernel<128, true, 1>, attend_kernel<128, true, 2>, attend_kernel<128, true, 0>}},
+    {{attend_kernel<256, false, 1>, attend_kernel<256, false, 2>, attend_kernel<256, false, 0>},
+     {attend_kernel<256, true, 1>, attend_kernel<256, true, 2>, attend_kernel<256, true, 0>}}};
 AttendKernel kernel_for(int32_t hd, bool e4m3, int32_t rows) {
     return kKernels[hd == 64 ? 0 : hd == 128 ? 1 : 2][e4m3][rows == 16 ? 0 : rows == 32 ? 1 : 2];
 }
@@ -1310,14 +1395,12 @@ hipError_t launch_attend(const AttendIn& in, const KvCacheIn& cache, bool e4m3, 
     const AttendWs aw{reinterpret_cast<WorkRange*>(p), reinterpret_cast<int32_t*>(p + w.done),
                       reinterpret_cast<float*>(p + w.parts)};
     const int64_t most = (static_cast<int64_t>(in.max_q) * (in.n_q / cache.n_kv) + rows - 1) / rows;
-    const int32_t least = rows == kTileRows ? 1 : 4, whole = rows == kTileRows ? kWholeUnit : 0;
-    const int32_t extra = rows == kTileRows ? kTileExtra : kRowExtra;
     if (most > 4)
         hipLaunchKernelGGL(attend_plan_kernel<true>, dim3(n_wg / (kPlanThreads / kWave)), dim3(kPlanThreads), 0,
-                           stream, in, cache, aw, rows, n_wg, least, whole, extra);
+                           stream, in, cache, aw, deal_of(rows), n_wg);
     else
         hipLaunchKernelGGL(attend_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, stream, in, cache, aw,
-                           rows, n_wg, least, whole, extra);
+                           deal_of(rows), n_wg);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel_for(cache.head_dim, e4m3, rows), dim3(n_wg), dim3(kAttendThreads), 0, stream,
