@@ -1345,10 +1345,13 @@ attend_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
 
 namespace {
 
-// Rows of a unit: all rows that a request can have where those are few.
+// Rows of a unit: all rows that a request can have where those are few.  64 requests
+// with 5 drafted tokens each, 4 heads to a key head: 102 us as units of 32 rows, 117
+// as tiles at head_dim 64, 185 and 230 at 128; at 256 their registers spill, and tiles
+// take as long in bf16 (396 us) and less in e4m3 (279 us for 325).
 int32_t unit_rows(int32_t n_q, int32_t max_q, const KvCacheIn& c) {
     const int64_t rows = static_cast<int64_t>(max_q) * (n_q / c.n_kv);
-    return rows <= 16 ? 16 : rows <= 32 ? 32 : kTileRows;
+    return rows <= 16 ? 16 : rows <= 32 && c.head_dim < 256 ? 32 : kTileRows;
 }
 // Workgroups of a launch: as many as the chip holds at a time (two on a CU where
 // their registers allow it).
@@ -1369,14 +1372,14 @@ WsLayout ws_layout(int32_t rows, const KvCacheIn& c) {
 }
 
 using AttendKernel = void (*)(AttendIn, KvCacheIn, AttendWs);
-// Indexed by head_dim (64, 128, 256), type and form (16 rows, 32 rows, tiles).
+// Indexed by head_dim (64, 128, 256), type and rows of a unit (16, 32, 128).
 constexpr AttendKernel kKernels[3][2][3] = {
     {{attend_kernel<64, false, 1>, attend_kernel<64, false, 2>, attend_kernel<64, false, 0>},
      {attend_kernel<64, true, 1>, attend_kernel<64, true, 2>, attend_kernel<64, true, 0>}},
     {{attend_kernel<128, false, 1>, attend_kernel<128, false, 2>, attend_kernel<128, false, 0>},
      {attend_kernel<128, true, 1>, attend_kernel<128, true, 2>, attend_kernel<128, true, 0>}},
-    {{attend_kernel<256, false, 1>, attend_kernel<256, false, 2>, attend_kernel<256, false, 0>},
-     {attend_kernel<256, true, 1>, attend_kernel<256, true, 2>, attend_kernel<256, true, 0>}}};
+    {{attend_kernel<256, false, 1>, nullptr, attend_kernel<256, false, 0>},
+     {attend_kernel<256, true, 1>, nullptr, attend_kernel<256, true, 0>}}};
 AttendKernel kernel_for(int32_t hd, bool e4m3, int32_t rows) {
     return kKernels[hd == 64 ? 0 : hd == 128 ? 1 : 2][e4m3][rows == 16 ? 0 : rows == 32 ? 1 : 2];
 }
@@ -1413,7 +1416,8 @@ void add_attend_kernels(std::vector<KernelInfo>& t) {
     t.push_back(kernel_info(attend_plan_kernel<true>));
     for (const auto& width : kKernels)
         for (const auto& type : width)
-            for (const AttendKernel k : type) t.push_back(kernel_info(k));
+            for (const AttendKernel k : type)
+                if (k) t.push_back(kernel_info(k));
 }
 
 }  // namespace xmix
