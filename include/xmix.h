@@ -674,7 +674,8 @@ xmix_status xmix_kv_append(const void *k, int64_t k_stride, const void *v, int64
  * parts that depend on the lengths of the whole batch and are joined in a fixed
  * order: equal calls give equal bits.
  * q [T_max, n_q, head_dim] bf16, out likewise, row strides in elements;
- * lse_out [n_q][T_max] fp32, or NULL.  Rows outside every span are not written.
+ * lse_out [n_q][T_max] fp32, or NULL; out and lse_out overlap nothing else.
+ * Rows outside every span are not written.
  * cu_seqlens [R_max + 1], kv_len [R_max] int32, device; max_q (host): no span
  * is longer.  A span outside [0, T_max] or longer than max_q, or a key count
  * outside [0, max_pages * page_size] of a request with tokens, sets

@@ -310,6 +310,7 @@ class Rope:
         if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1:
             raise TypeError("inv_freq must be a float64 vector")
         self.inv_freq, self.rot_dim, self.pairing = inv_freq, 2 * inv_freq.numel(), int(pairing)
+        self.device = inv_freq.device
         self.struct = XmixRope(_ptr(inv_freq), self.rot_dim, self.pairing)
 
 
@@ -714,6 +715,12 @@ def xmix_readback_compact(segments: Sequence[torch.Tensor], route: Route, app_bi
         app_id, ctypes.byref(ring.struct), _stream(stream)))
 
 
+def _beside(t, *held):
+    """The objects' tensors live on the device of `t`."""
+    if any(x is not None and x.device != t.device for x in held):
+        raise ValueError("the cache and the rotation must live on the tensors' device")
+
+
 def xmix_qk_norm_rope(q, k, pos_of_token, q_weight, k_weight, eps: float, rope: Optional[Rope],
                       q_out, k_out, T_valid=None, stream=None):
     """Norm of every head (weight [head_dim]; None: none) and position rotation
@@ -721,6 +728,7 @@ def xmix_qk_norm_rope(q, k, pos_of_token, q_weight, k_weight, eps: float, rope: 
     bf16/fp32 (k and k_out None: queries alone) into q_out and k_out, which may be
     q and k.  Rows may lie any distance apart; pos_of_token int32 [T_max], a
     negative one leaves its row out."""
+    _beside(q, rope)
     _check("xmix_qk_norm_rope", _qk_norm_rope(q, k, pos_of_token, q_weight, k_weight, eps, rope,
                                               q_out, k_out, T_valid, stream))
 
@@ -729,6 +737,7 @@ def xmix_kv_append(k, v, req_of_token, pos_of_token, rope: Optional[Rope], cache
                    T_valid=None, stream=None):
     """The keys (rotated by `rope`; None: as they are) and values of a step,
     [T_max, n_kv, head_dim] bf16/fp32, into the pages of their requests."""
+    _beside(k, rope, cache)
     _check("xmix_kv_append", _kv_append(k, v, req_of_token, pos_of_token, rope, cache, cache.n_kv,
                                         cache.head_dim, err_word, T_valid, stream))
 
@@ -745,6 +754,7 @@ def xmix_paged_attention(q, cu_seqlens, kv_len, cache: KvCache, scale: float, wi
     among them); window: the keys a token sees at most, itself among them (0: all);
     max_q: no span is longer; ws: uint8, paged_attention_workspace bytes."""
     assert cu_seqlens.numel() == cache.R_max + 1
+    _beside(q, cache)
     _check("xmix_paged_attention", _paged_attention(
         q, cu_seqlens, kv_len, cache, cache.R_max, cache.head_dim, scale, window, max_q, out,
         lse_out, err_word, ws, stream))

@@ -23,6 +23,16 @@ struct ArgPointers<HeadRows> {
 };
 constexpr int kHeadThreads = 256;
 
+// A workgroup per token, in rows of the grid: the threads of one dimension of a grid
+// number less than 2^32, 16.7 million tokens.
+constexpr int32_t kGridTokens = 1 << 20;
+__device__ __forceinline__ int32_t grid_token() {
+    return static_cast<int32_t>(blockIdx.y * kGridTokens + blockIdx.x);
+}
+inline dim3 token_grid(int32_t T_max) {
+    return T_max <= kGridTokens ? dim3(T_max) : dim3(kGridTokens, (T_max - 1) / kGridTokens + 1);
+}
+
 // Sum over the n lanes (a power of two up to 16) that share a head.
 __device__ __forceinline__ float head_sum(float v, int n) {
     if (n > 1) v += dpp_f<kDppXor1>(v);
@@ -38,10 +48,12 @@ __device__ __forceinline__ float head_sum(float v, int n) {
 //   y = x (mean(x^2) + eps)^(-1/2) w,   out = round(rotate(y))
 template <bool BF16>
 __global__ void __launch_bounds__(kHeadThreads)
-norm_rope_kernel(HeadRows q, HeadRows k, int32_t head_dim, int32_t lanes_log2,
+norm_rope_kernel(HeadRows q, HeadRows k, int32_t head_dim, int32_t lanes_log2, int32_t T_max,
                  const int32_t* __restrict__ pos_of_token, const int32_t* __restrict__ T_valid,
                  float eps, RopeIn rope) {
-    const int32_t t = blockIdx.x, pos = pos_of_token[t];
+    const int32_t t = grid_token();
+    if (t >= T_max) return;
+    const int32_t pos = pos_of_token[t];
     if (pos < 0 || (T_valid && t >= *T_valid)) return;
     const int lanes = 1 << lanes_log2, u = threadIdx.x & (lanes - 1);
     const bool mine = 2 * kChunk * u < head_dim;
@@ -91,11 +103,11 @@ hipError_t launch_norm_rope(const HeadRows& q, const HeadRows& k, bool bf16, int
     int lg = 0;
     while ((1 << lg) < head_lanes(head_dim)) ++lg;
     if (bf16)
-        hipLaunchKernelGGL(norm_rope_kernel<true>, dim3(T_max), dim3(kHeadThreads), 0, stream, q, k,
-                           head_dim, lg, pos, T_valid, eps, rope);
+        hipLaunchKernelGGL(norm_rope_kernel<true>, token_grid(T_max), dim3(kHeadThreads), 0, stream, q,
+                           k, head_dim, lg, T_max, pos, T_valid, eps, rope);
     else
-        hipLaunchKernelGGL(norm_rope_kernel<false>, dim3(T_max), dim3(kHeadThreads), 0, stream, q, k,
-                           head_dim, lg, pos, T_valid, eps, rope);
+        hipLaunchKernelGGL(norm_rope_kernel<false>, token_grid(T_max), dim3(kHeadThreads), 0, stream, q,
+                           k, head_dim, lg, T_max, pos, T_valid, eps, rope);
     return hipGetLastError();
 }
 
@@ -116,10 +128,12 @@ __device__ __forceinline__ uint32_t pack4_e4m3(const float* x) {
 template <bool BF16, bool E4M3>
 __global__ void __launch_bounds__(kHeadThreads)
 kv_append_kernel(const void* __restrict__ k, int64_t k_stride, const void* __restrict__ v,
-                 int64_t v_stride, int32_t lanes_log2, const int32_t* __restrict__ req_of_token,
+                 int64_t v_stride, int32_t lanes_log2, int32_t T_max, const int32_t* __restrict__ req_of_token,
                  const int32_t* __restrict__ pos_of_token, const int32_t* __restrict__ T_valid,
                  RopeIn rope, KvCacheIn cache, uint32_t* __restrict__ err_word) {
-    const int32_t t = blockIdx.x, req = req_of_token[t], pos = pos_of_token[t];
+    const int32_t t = grid_token();
+    if (t >= T_max) return;
+    const int32_t req = req_of_token[t], pos = pos_of_token[t];
     if (req < 0 || pos < 0 || (T_valid && t >= *T_valid)) return;
     int32_t page = -1;
     const int32_t nth = pos >> cache.page_log2;
@@ -172,8 +186,8 @@ hipError_t launch_kv_append(const void* k, int64_t k_stride, const void* v, int6
     while ((1 << lg) < head_lanes(cache.head_dim)) ++lg;
     const auto kernel = bf16 ? (e4m3 ? kv_append_kernel<true, true> : kv_append_kernel<true, false>)
                              : (e4m3 ? kv_append_kernel<false, true> : kv_append_kernel<false, false>);
-    hipLaunchKernelGGL(kernel, dim3(T_max), dim3(kHeadThreads), 0, stream, k, k_stride, v, v_stride,
-                       lg, req, pos, T_valid, rope, cache, err_word);
+    hipLaunchKernelGGL(kernel, token_grid(T_max), dim3(kHeadThreads), 0, stream, k, k_stride, v,
+                       v_stride, lg, T_max, req, pos, T_valid, rope, cache, err_word);
     return hipGetLastError();
 }
 
