@@ -56,6 +56,8 @@ constexpr int kTileRows = 128;     // rows of a tile unit
 constexpr int kFewRows = 16;       // rows of a request that are a row unit among tiles
 constexpr int kMaxRequests = 4096, kMaxRanges = 512;
 constexpr int kPlanThreads = 1024;
+constexpr int kPlanRanges = 8;     // of one workgroup, and the start of the next one's
+constexpr int kTilesEach = 4;      // tiles of a request that one thread walks over
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 // A running maximum is raised only by a score this far above it (powers of two): the
 // weights stay below 2^8, which neither fp32 sums nor bf16 weights mind, and the
@@ -105,6 +107,13 @@ struct ArgPointers<AttendWs> {
 };
 
 // ------------------------------------------------------------------- geometry
+
+// a / b of numbers that are not negative: 64 bits are divided in some 150 instructions,
+// and few batches need them.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+    return a / b;
+}
 
 // A value that nothing writes during the launch, at a uniform place: a scalar load,
 // which waits for no vector load before it (a page id behind the copies of the
@@ -171,40 +180,58 @@ __device__ __forceinline__ int64_t wave_sum64(int64_t v) {
 }
 
 // Blocks of each request, their prefix, then the start of every range by a search in
-// the prefix and among the request's tiles.  Where a request has few tiles, one
-// workgroup with a thread a request and a thread a range; where it may have MANY, a
-// wave each, and as many workgroups as there are ranges for (all find the same
-// prefix): walking over 64 tiles a thread took 25 us on the one CU.  A range that would
-// begin inside a short tile unit (up to `whole` blocks) begins at the nearer end of it
-// instead: its parts would take their way through memory, 64 KB each, and sixteen
-// prompts of 128 to 1024 tokens took 245 us with every end cut and 211 so.
+// the prefix and among the request's tiles.  Where no request can have more than
+// kTilesEach tiles, one workgroup with a thread a request and a thread a range; where
+// one may (MANY), a wave for each that does and a wave a range, with as many
+// workgroups as there are ranges for (all find the same prefix): walking over 64 tiles
+// a thread took 25 us on the one CU.  Chains of round trips and of 64-bit divisions
+// are what it costs: 8 us with the spans in LDS and short divisions (11 before) in a
+// batch of 96 requests, 3 us for one request.
+//
+// A range that would begin inside a short tile unit (up to `whole` blocks) begins at
+// the nearer end of it instead: its parts would take their way through memory, 64 KB
+// each, and sixteen prompts of 128 to 1024 tokens took 245 us with every end cut and
+// 211 so.
 template <bool MANY>
 __global__ void __launch_bounds__(kPlanThreads)
 attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t n_wg) {
+    __shared__ Span spans[kMaxRequests];
     __shared__ int64_t upto[kMaxRequests + 1], begins[kMaxRanges + 1];
     __shared__ int64_t wave_total[kPlanThreads / kWave];
     __shared__ uint64_t tile_ranges[kMaxRanges / kWave];
+    __shared__ uint16_t many[MANY ? kMaxRequests : 1];  // requests of many tiles
+    __shared__ int n_many;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int32_t R = cache.R_max;
     const HeadGroup group = in.group;
     const int32_t rows = deal.rows, extra = deal.extra;
     auto step_of = [&](int32_t n) { return few_rows(n, group) ? deal.few_step : deal.step; };
+    auto place_of = [&](const Span& s, int32_t t, int32_t step) {
+        return blocks_of(s, t, group, rows, in.window).count * step + extra;
+    };
+    if (MANY && tid == 0) n_many = 0;
+    __syncthreads();
     bool bad = false;
-    if constexpr (!MANY) {
-        for (int32_t r = tid; r < R; r += kPlanThreads) {
-            const Span s = span_of(in, cache, r, &bad);
-            const int32_t tiles = tiles_of(s.n, group, rows), step = step_of(s.n);
-            int64_t sum = 0;
-            for (int32_t t = 0; t < tiles; ++t) sum += blocks_of(s, t, group, rows, in.window).count * step + extra;
-            upto[r + 1] = sum * cache.n_kv;
+    for (int32_t r = tid; r < R; r += kPlanThreads) {
+        const Span s = span_of(in, cache, r, &bad);
+        spans[r] = s;
+        const int32_t tiles = tiles_of(s.n, group, rows), step = step_of(s.n);
+        if (MANY && tiles > kTilesEach) {
+            many[atomicAdd(&n_many, 1)] = static_cast<uint16_t>(r);
+            continue;
         }
-    } else {
-        for (int32_t r = wave; r < R; r += kPlanThreads / kWave) {
-            const Span s = span_of(in, cache, r, &bad);
+        int64_t sum = 0;
+        for (int32_t t = 0; t < tiles; ++t) sum += place_of(s, t, step);
+        upto[r + 1] = sum * cache.n_kv;
+    }
+    if constexpr (MANY) {
+        __syncthreads();
+        for (int32_t i = wave; i < n_many; i += kPlanThreads / kWave) {
+            const int32_t r = many[i];
+            const Span s = spans[r];
             const int32_t tiles = tiles_of(s.n, group, rows), step = step_of(s.n);
             int64_t sum = 0;
-            for (int32_t t = lane; t < tiles; t += kWave)
-                sum += blocks_of(s, t, group, rows, in.window).count * step + extra;
+            for (int32_t t = lane; t < tiles; t += kWave) sum += place_of(s, t, step);
             sum = wave_sum64(sum);
             if (lane == 0) upto[r + 1] = sum * cache.n_kv;
         }
@@ -233,7 +260,7 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t
         if (tid * kEach + i < R) upto[tid * kEach + i + 1] = before + v[i];
     __syncthreads();
     const int64_t places = upto[R];
-    const int64_t share = max(static_cast<int64_t>(deal.least), (places + n_wg - 1) / n_wg);
+    const int64_t share = max(static_cast<int64_t>(deal.least), quotient(places + n_wg - 1, n_wg));
     // The last request that starts at or before a place.
     auto request_at = [&](int64_t at) {
         int32_t lo = 0, hi = R - 1;
@@ -247,10 +274,11 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t
     // The unit and its block at position `at` (uniform where MANY), and the unit's blocks.
     auto locate = [&](int64_t at, int32_t* count) {
         const int32_t lo = request_at(at);
-        const Span s = span_of(in, cache, lo);
-        const int64_t a_head = (upto[lo + 1] - upto[lo]) / cache.n_kv, rest = at - upto[lo];
-        WorkRange st{at, 0, share, lo, static_cast<int32_t>(rest / a_head), 0, 0, s.lo, s.n, s.len, 0};
-        int64_t left = rest % a_head;
+        const Span s = spans[lo];
+        const int64_t a_head = quotient(upto[lo + 1] - upto[lo], cache.n_kv), rest = at - upto[lo];
+        const int32_t head = static_cast<int32_t>(quotient(rest, a_head));
+        WorkRange st{at, 0, share, lo, head, 0, 0, s.lo, s.n, s.len, 0};
+        int64_t left = rest - head * a_head;
         const int32_t tiles = tiles_of(s.n, group, rows), step = step_of(s.n);
         *count = 1;
         if constexpr (MANY) {  // 64 tiles at a time
@@ -306,7 +334,7 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t
     // tiles first, such that a CU, whose second workgroup is 32 behind its first, has
     // both: 95 single tokens and a chunk of 1001 take 134 us so, 140 with the ranges
     // in their order and 161 with the rows first.
-    const int32_t used = static_cast<int32_t>(min(static_cast<int64_t>(n_wg), (places + share - 1) / share));
+    const int32_t used = static_cast<int32_t>(min(static_cast<int64_t>(n_wg), quotient(places + share - 1, share)));
     const int32_t each = (used + 7) / 8;
     const bool mixed = deal.step != deal.few_step;
     if (mixed) {
@@ -314,7 +342,7 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t
             bool tile = false;
             if (tid < used) {
                 const int32_t r = request_at(tid * share);
-                tile = !few_rows(in.cu[r + 1] - in.cu[r], group);
+                tile = !few_rows(spans[r].n, group);
             }
             const uint64_t mask = wave_ballot(tile);
             if (lane == 0) tile_ranges[wave] = mask;
@@ -354,14 +382,13 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t
         ws.range[workgroup_of(w)] = st;
     };
     if constexpr (MANY) {  // a wave a range
-        const WorkRange st = begin_of(w0 + wave);
-        if (lane == 0) note_begin(wave, st);
-        if (wave == 0) {
-            const WorkRange last = begin_of(w0 + per);
-            if (lane == 0) note_begin(per, last);
+        WorkRange st;
+        if (wave <= per) {
+            st = begin_of(w0 + wave);
+            if (lane == 0) note_begin(wave, st);
         }
         __syncthreads();
-        if (lane == 0) put_range(wave, st);
+        if (wave < per && lane == 0) put_range(wave, st);
     } else {  // a thread a range
         WorkRange st;
         if (tid <= per) {
@@ -960,8 +987,8 @@ __device__ __forceinline__ void tile_unit(const AttendIn& in, const KvCacheIn& c
         careful = true;
     }
     if (count != bl.count) {
-        join_parts<kTileRows, HD, kTileRows>(in, ws, u, static_cast<int32_t>(begin / st.share),
-                                  static_cast<int32_t>(last / st.share), v_scale, lds.flag);
+        join_parts<kTileRows, HD, kTileRows>(in, ws, u, static_cast<int32_t>(quotient(begin, st.share)),
+                                  static_cast<int32_t>(quotient(last, st.share)), v_scale, lds.flag);
     }
 }
 
@@ -1283,8 +1310,8 @@ __device__ __forceinline__ void row_unit(const AttendIn& in, const KvCacheIn& ca
     if (!whole) {
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
-        join_parts<M, HD, SLOT>(in, ws, u, static_cast<int32_t>(begin / st.share),
-                          static_cast<int32_t>(last / st.share), v_scale, lds.flag);
+        join_parts<M, HD, SLOT>(in, ws, u, static_cast<int32_t>(quotient(begin, st.share)),
+                          static_cast<int32_t>(quotient(last, st.share)), v_scale, lds.flag);
     }
     __syncthreads();  // before V is copied in again
 }
@@ -1398,8 +1425,8 @@ hipError_t launch_attend(const AttendIn& in, const KvCacheIn& cache, bool e4m3, 
     const AttendWs aw{reinterpret_cast<WorkRange*>(p), reinterpret_cast<int32_t*>(p + w.done),
                       reinterpret_cast<float*>(p + w.parts)};
     const int64_t most = (static_cast<int64_t>(in.max_q) * (in.n_q / cache.n_kv) + rows - 1) / rows;
-    if (most > 4)
-        hipLaunchKernelGGL(attend_plan_kernel<true>, dim3(n_wg / (kPlanThreads / kWave)), dim3(kPlanThreads), 0,
+    if (most > kTilesEach)
+        hipLaunchKernelGGL(attend_plan_kernel<true>, dim3(n_wg / kPlanRanges), dim3(kPlanThreads), 0,
                            stream, in, cache, aw, deal_of(rows), n_wg);
     else
         hipLaunchKernelGGL(attend_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, stream, in, cache, aw,
