@@ -15,9 +15,10 @@
 //
 // Work is dealt in blocks of 64 keys.  A unit is one key head of one request and a
 // tile of its rows; the blocks of all units, one behind the other and weighed by what
-// they cost, are cut into equal ranges, one per workgroup, whatever the lengths are.  A unit that is cut leaves a
-// part (maximum, sum, O) per workgroup in the workspace, and the last workgroup to
-// finish one joins them in order.  attend_plan_kernel finds where each range starts.
+// they cost, are cut into equal ranges, one per workgroup, whatever the lengths are.
+// A unit that is cut leaves a part (maximum, sum, O) per workgroup in the workspace,
+// and the last workgroup to finish one joins them in order.  attend_plan_kernel finds
+// where each range starts.
 //
 // Two kinds of unit, each with an inner loop of its own:
 //   tile unit   128 rows; the workgroup's four waves take 32 rows each and share K
@@ -69,7 +70,7 @@ constexpr float kRaise = 8.0f;
 struct WorkRange {
     int64_t at;                      // place of the unit it begins in
     int64_t end;                     // where it ends
-    int64_t share;                   // blocks of a range before its ends were moved
+    int64_t share;                   // places of a range before its ends were moved
     int32_t req, head, tile, block;  // the unit, and its block that is the first
     int32_t lo, n, len;              // the request's span and keys
     int32_t nth;                     // its place among the ranges
@@ -85,7 +86,10 @@ struct Deal {
     int32_t whole;                  // tiles of so many blocks are not cut
 };
 // A block of a tile takes half as long again as one of a row unit (1.4 us and 0.9 us
-// at head_dim 64, two workgroups on a CU), a unit's own cost is 4 to 8 us.
+// at head_dim 64, two workgroups on a CU), a unit's own cost is 6 to 8 us; sixteen
+// prompts take 145 us with 9 places for it, 150 with 12 and 148 with 15.  A launch of
+// row units alone takes 643 us with 4 (256 requests of up to 8192 keys), 640 with 2,
+// 652 with 8; one request of 1024 keys 16.0, 18.7 and 16.1.
 constexpr Deal kDealRows = {0, 4, 1, 1, 4, 0}, kDealTiles = {kTileRows, 9, 3, 2, 3, 18};
 __host__ __device__ constexpr Deal deal_of(int32_t rows) {
     Deal d = rows == kTileRows ? kDealTiles : kDealRows;
@@ -332,7 +336,7 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t
     // ranges still to all of them; but tiles, which keep the matrix units busy, and
     // rows, which wait for memory, are spread over the XCDs each on their own, the
     // tiles first, such that a CU, whose second workgroup is 32 behind its first, has
-    // both: 95 single tokens and a chunk of 1001 take 134 us so, 140 with the ranges
+    // both: 95 single tokens and a chunk of 1001 took 134 us so, 140 with the ranges
     // in their order and 161 with the rows first.
     const int32_t used = static_cast<int32_t>(min(static_cast<int64_t>(n_wg), quotient(places + share - 1, share)));
     const int32_t each = (used + 7) / 8;
@@ -603,8 +607,8 @@ __device__ __forceinline__ f32x4_t load4_through(__amdgpu_buffer_rsrc_t r, int o
 // with room for SLOT rows.
 // Parts pass between XCDs, whose L2 caches do not see each other's writes: they are
 // stored through to memory and loaded from there (sc1), which needs no fence.  An
-// agent fence writes the whole L2 back, a good half microsecond each, one
-// after the other: a call of 32 workgroups took 33 us with them and 10 without.
+// agent fence writes the whole L2 back, a good half microsecond each, one after the
+// other: one request of 1024 keys took 37.8 us with them and 16.7 without.
 template <int M, int HD, int SLOT>
 struct Part {
     static constexpr int kFloats = SLOT * (HD + 2);
@@ -687,6 +691,9 @@ __device__ __forceinline__ void join_rows(const AttendIn& in, const AttendWs& ws
 template <int M, int HD, int SLOT>
 __device__ void join_parts(const AttendIn& in, const AttendWs& ws, const RowsOut& u, int32_t first,
                            int32_t last, float v_scale, int* flag) {
+    // (in the workspace also if a caller changes the lengths under the call)
+    last = min(last, static_cast<int32_t>(gridDim.x) - 1);
+    first = min(first, last);
     if (threadIdx.x == 0)
         *flag = __hip_atomic_fetch_add(ws.done + first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
                 last - first;
@@ -716,7 +723,17 @@ struct UnitLds {
 };
 
 // `count` blocks from the range's on of a unit of 128 rows, whose first and last block
-// are at the places `begin` and `last`.
+// are at the places `begin` and `last`.  A wave's 32 rows are one side of a 32 x 32
+// product; K and V of a block come by copies into LDS, the block behind it while this
+// one is multiplied, and every operand read from there serves 32 rows.
+//
+// The matrix units and the device's power bound it: 4096 tokens over 32768 keys, 32
+// heads of 128, run at 930 to 990 TFLOP/s (2.1 to 2.2 ms; 53 % of the cycles in matrix
+// instructions, the library's plain product reaches 1249).  With few blocks a unit
+// its start does, the chain from page id to copy to first product: units of one block
+// take 9 us, of eight 18 (sixteen prompts of up to 1024 tokens: 145 us, 470 TFLOP/s).
+// The next unit's first copies issued before this one's rows are stored did not help
+// (147 to 159 us), the CU's second workgroup being at work meanwhile.
 template <int HD, bool E4M3>
 __device__ __forceinline__ void tile_unit(const AttendIn& in, const KvCacheIn& cache, const AttendWs& ws,
                                           const WorkRange& st, const Span& s, const Blocks& bl,
@@ -1001,7 +1018,15 @@ struct RowStep {
     static constexpr int kTile = kKeys * HD * (E4M3 ? 1 : 2) / 16;
 };
 
-// The same of a unit of 16 NB rows; SLOT: rows that a part has room for.
+// The same of a unit of 16 NB rows; SLOT: rows that a part has room for.  Each wave
+// takes every fourth step of 32 or 64 keys by itself: K from memory into the registers
+// that the product takes it from, V through LDS of the wave's own, both a step ahead.
+//
+// Memory bounds it: 256 requests of up to 8192 keys, heads of 128, read 4.1 GB (what
+// they hold, by the counters too) in 643 us, 6.4 TB/s of the 7.0 that a plain read
+// reaches; in e4m3 2.0 GB take 320 us, 6.3 TB/s; with 32 rows a unit (five tokens a
+// request, a window of 4096) 0.84 GB take 177 to 189 us, where a unit's start, its
+// parts and their join are 17 to 20 us of about 130.
 template <int HD, bool E4M3, int NB, int SLOT>
 __device__ __forceinline__ void row_unit(const AttendIn& in, const KvCacheIn& cache, const AttendWs& ws,
                                          const WorkRange& st, const Span& s, const Blocks& bl,
