@@ -136,3 +136,30 @@ def test_rows_and_tiles_in_one_call(px, hd, n_kv, group, window):
     ws.fill_(0x5A)
     px.xmix_paged_attention(q, cu, i32(ln), cache, scale, window, 200, again, None, err, ws)
     assert same(out, again)
+
+
+@pytest.mark.parametrize("dtype", [BF, torch.float32])
+def test_scaled_values_are_the_rounded_quotients(px, dtype):
+    """Keys and values of every exponent over scales from 2^-80 to 2^80 and ones that
+    are no powers of two, to the bit (signs of zeros too)."""
+    n_kv, hd, T, ps = 16, 64, 512, 16
+    rng = np.random.default_rng(4)
+    x = rng.normal(size=(T, n_kv, hd)) * 2.0 ** rng.integers(-20, 20, (T, n_kv, 1))
+    scale = np.float32(rng.uniform(1, 2, n_kv) * 2.0 ** np.linspace(-80, 80, n_kv))
+    scale[[3, 8]] = 0.0375, 1.0
+    x = x * scale[:, None].astype(np.float64) * 2.0 ** rng.integers(-6, 7, (T, 1, 1))
+    x[::7] = rng.normal(size=x[::7].shape) * 2.0 ** rng.integers(-120, 120, x[::7].shape)
+    x[0], x[1], x[2], x[3] = 0.0, -0.0, 3e38, -1e-38
+    x[4] = (rng.integers(-448, 449, (n_kv, hd)) / 16.0) * scale[:, None]  # ties among them
+    k = torch.as_tensor(x).to(dtype).cuda()
+    s = torch.as_tensor(scale).cuda()
+    pages = torch.arange(T // ps, dtype=torch.int32, device="cuda")[None].contiguous()
+    cache = px.KvCache(*[torch.zeros(T // ps, n_kv, ps, hd, device="cuda").to(torch.float8_e4m3fn) for _ in "kv"],
+                       pages, s, s)
+    err = i32([0])
+    px.xmix_kv_append(k, k, i32(np.zeros(T)), i32(np.arange(T)), None, cache, err)
+    want = (k.float().cpu() / s.cpu()[:, None]).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+    for got in (cache.k, cache.v):
+        rows = got.view(torch.uint8).cpu().transpose(1, 2).reshape(T, n_kv, hd)
+        assert torch.equal(rows, want)
+    assert int(err.item()) == 0
