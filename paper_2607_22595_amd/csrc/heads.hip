@@ -2,8 +2,7 @@
 // queries and keys, and the append of keys and values to the paged cache.
 //
 // Both read every value once and write it once, so memory bounds them (and at
-// decode sizes the latency of one chain: position, rows, result).  One workgroup per
-// token lets a lane compute its angles once for all heads of the token.
+// decode sizes the latency of one chain: position, rows, result).
 #include "common.hpp"
 #include "kernels.hpp"
 #include "launch.hpp"
@@ -24,14 +23,26 @@ struct ArgPointers<HeadRows> {
 };
 constexpr int kHeadThreadsLog2 = 8, kHeadThreads = 1 << kHeadThreadsLog2;
 
-// A workgroup per token, in rows of the grid: the threads of one dimension of a grid
-// number less than 2^32, 16.7 million tokens.
-constexpr int32_t kGridTokens = 1 << 20;
-__device__ __forceinline__ int32_t grid_token() {
-    return static_cast<int32_t>(blockIdx.y * kGridTokens + blockIdx.x);
+// The workgroup's place, in rows of the grid: the threads of one dimension of a grid
+// number less than 2^32.
+constexpr int32_t kGridRow = 1 << 20;
+__device__ __forceinline__ int32_t grid_place() {
+    return static_cast<int32_t>(blockIdx.y * kGridRow + blockIdx.x);
 }
-inline dim3 token_grid(int32_t T_max) {
-    return T_max <= kGridTokens ? dim3(T_max) : dim3(kGridTokens, (T_max - 1) / kGridTokens + 1);
+// A token has the threads that its heads need, a power of two and a workgroup's at most:
+// 9982 tokens of one key and one value head took 10.5 us with a workgroup each, 4.4 so.
+struct TokenThreads {
+    int32_t lanes_log2, threads_log2;  // of a head, of a token
+    dim3 grid;
+};
+inline TokenThreads token_threads(int32_t head_dim, int32_t heads, int32_t T_max) {
+    TokenThreads n{0, 0, dim3()};
+    while ((1 << n.lanes_log2) < head_lanes(head_dim)) ++n.lanes_log2;
+    n.threads_log2 = n.lanes_log2;
+    while (n.threads_log2 < kHeadThreadsLog2 && (1 << (n.threads_log2 - n.lanes_log2)) < heads) ++n.threads_log2;
+    const int32_t groups = ((T_max - 1) >> (kHeadThreadsLog2 - n.threads_log2)) + 1;
+    n.grid = groups <= kGridRow ? dim3(groups) : dim3(kGridRow, (groups - 1) / kGridRow + 1);
+    return n;
 }
 
 // Sum over the n lanes (a power of two up to 16) that share a head.
@@ -43,38 +54,48 @@ __device__ __forceinline__ float head_sum(float v, int n) {
     return v;
 }
 
-// One workgroup per token.  Its lanes form groups of one head each, which take
-// the token's query heads and then its key heads in turn; a lane's angles are
-// computed once for all of them.
+// The token's lanes form groups of one head each, which take its query heads and then
+// its key heads in turn, the next head's rows on their way while one is worked on; a
+// lane's angles are computed once for all of them.
 //   y = x (mean(x^2) + eps)^(-1/2) w,   out = round(rotate(y))
-// 8192 tokens of 64 + 8 heads of 128: 62 to 64 us for 302 MB, 4.8 TB/s, the rate of a
-// large copy.  256 tokens of 32 + 8: 5.0 us, launch and one round trip.
+// 8192 tokens of 64 + 8 heads of 128: 49.8 us for 302 MB, 6.1 TB/s (61.6 us with a
+// head loaded after the one before it was stored); 256 tokens of 32 + 8: 4.7 us,
+// launch and one round trip.
 template <bool BF16>
 __global__ void __launch_bounds__(kHeadThreads)
-norm_rope_kernel(HeadRows q, HeadRows k, int32_t head_dim, int32_t lanes_log2, int32_t T_max,
-                 const int32_t* __restrict__ pos_of_token, const int32_t* __restrict__ T_valid,
-                 float eps, RopeIn rope) {
-    const int32_t t = grid_token();
-    if (t >= T_max) return;
-    const int32_t pos = pos_of_token[t];
-    if (pos < 0 || (T_valid && t >= *T_valid)) return;
-    const int lanes = 1 << lanes_log2, u = threadIdx.x & (lanes - 1);
+norm_rope_kernel(HeadRows q, HeadRows k, int32_t head_dim, int32_t lanes_log2, int32_t threads_log2,
+                 int32_t T_max, const int32_t* __restrict__ pos_of_token,
+                 const int32_t* __restrict__ T_valid, float eps, RopeIn rope) {
+    const int tid = threadIdx.x & ((1 << threads_log2) - 1);  // of the token's
+    const int64_t at = (static_cast<int64_t>(grid_place()) * kHeadThreads + threadIdx.x) >> threads_log2;
+    if (at >= T_max) return;
+    const int32_t t = static_cast<int32_t>(at);
+    const int lanes = 1 << lanes_log2, u = tid & (lanes - 1), heads = (1 << threads_log2) >> lanes_log2;
     const bool mine = 2 * kChunk * u < head_dim;
     const HeadPart part = head_part(u, rope);
+    constexpr int kBytes = BF16 ? 2 : 4;
+    auto load = [&](int h, Raw<BF16>* a, Raw<BF16>* b) {
+        const HeadRows& r = h < q.n ? q : k;
+        const char* x = static_cast<const char*>(r.x) +
+                        (t * r.stride + (h < q.n ? h : h - q.n) * static_cast<int64_t>(head_dim)) * kBytes;
+        *a = load_chunk<BF16>(x, part.a);
+        *b = load_chunk<BF16>(x, part.b);
+    };
+    int h = tid >> lanes_log2;
+    Raw<BF16> ra = {}, rb = {};
+    if (mine && h < q.n + k.n) load(h, &ra, &rb);  // on their way while the position is looked up
+    const int32_t pos = pos_of_token[t];
+    if (pos < 0 || (T_valid && t >= *T_valid)) return;
     Angles g;
     if (part.turned) angles(g, rope, u, pos);
-    constexpr int kBytes = BF16 ? 2 : 4;
-    for (int h = threadIdx.x >> lanes_log2; h < q.n + k.n; h += kHeadThreads >> lanes_log2) {
-        const bool is_q = h < q.n;
-        const HeadRows& r = is_q ? q : k;
-        const int64_t in_row = (is_q ? h : h - q.n) * static_cast<int64_t>(head_dim);
-        const char* x = static_cast<const char*>(r.x) + (t * r.stride + in_row) * kBytes;
-        float a[kChunk] = {}, b[kChunk] = {};
-        if (mine) {
-            const Raw<BF16> ra = load_chunk<BF16>(x, part.a), rb = load_chunk<BF16>(x, part.b);
-            widen<BF16>(ra, a);
-            widen<BF16>(rb, b);
-        }
+    while (h < q.n + k.n) {
+        const HeadRows& r = h < q.n ? q : k;
+        const int64_t row = (h < q.n ? h : h - q.n) * static_cast<int64_t>(head_dim);
+        float a[kChunk], b[kChunk];
+        widen<BF16>(ra, a);
+        widen<BF16>(rb, b);
+        h += heads;
+        if (mine && h < q.n + k.n) load(h, &ra, &rb);
         if (r.weight) {
             float sum = 0.0f;
 #pragma unroll
@@ -94,7 +115,7 @@ norm_rope_kernel(HeadRows q, HeadRows k, int32_t head_dim, int32_t lanes_log2, i
         }
         if (!mine) continue;
         if (part.turned) rotate(a, b, g, rope.pairs != 0);
-        char* out = static_cast<char*>(r.out) + (t * r.out_stride + in_row) * kBytes;
+        char* out = static_cast<char*>(r.out) + (t * r.out_stride + row) * kBytes;
         store_chunk<BF16>(out, part.a, a);
         store_chunk<BF16>(out, part.b, b);
     }
@@ -103,14 +124,9 @@ norm_rope_kernel(HeadRows q, HeadRows k, int32_t head_dim, int32_t lanes_log2, i
 hipError_t launch_norm_rope(const HeadRows& q, const HeadRows& k, bool bf16, int32_t head_dim,
                             int32_t T_max, const int32_t* pos, const int32_t* T_valid, float eps,
                             const RopeIn& rope, hipStream_t stream) {
-    int lg = 0;
-    while ((1 << lg) < head_lanes(head_dim)) ++lg;
-    if (bf16)
-        hipLaunchKernelGGL(norm_rope_kernel<true>, token_grid(T_max), dim3(kHeadThreads), 0, stream, q,
-                           k, head_dim, lg, T_max, pos, T_valid, eps, rope);
-    else
-        hipLaunchKernelGGL(norm_rope_kernel<false>, token_grid(T_max), dim3(kHeadThreads), 0, stream, q,
-                           k, head_dim, lg, T_max, pos, T_valid, eps, rope);
+    const TokenThreads n = token_threads(head_dim, q.n + k.n, T_max);
+    hipLaunchKernelGGL(bf16 ? norm_rope_kernel<true> : norm_rope_kernel<false>, n.grid, dim3(kHeadThreads), 0,
+                       stream, q, k, head_dim, n.lanes_log2, n.threads_log2, T_max, pos, T_valid, eps, rope);
     return hipGetLastError();
 }
 
@@ -163,7 +179,7 @@ kv_append_kernel(const void* __restrict__ k, int64_t k_stride, const void* __res
                  const int32_t* __restrict__ T_valid, RopeIn rope, KvCacheIn cache,
                  uint32_t* __restrict__ err_word) {
     const int tid = threadIdx.x & ((1 << threads_log2) - 1);  // of the token's
-    const int64_t at = (static_cast<int64_t>(grid_token()) * kHeadThreads + threadIdx.x) >> threads_log2;
+    const int64_t at = (static_cast<int64_t>(grid_place()) * kHeadThreads + threadIdx.x) >> threads_log2;
     if (at >= T_max) return;
     const int32_t t = static_cast<int32_t>(at), hd = cache.head_dim;
     const int lanes = 1 << lanes_log2, u = tid & (lanes - 1), heads = (1 << threads_log2) >> lanes_log2;
@@ -221,15 +237,11 @@ hipError_t launch_kv_append(const void* k, int64_t k_stride, const void* v, int6
                             bool bf16, int32_t T_max, const int32_t* req, const int32_t* pos,
                             const int32_t* T_valid, const RopeIn& rope, const KvCacheIn& cache,
                             bool e4m3, uint32_t* err_word, hipStream_t stream) {
-    int lg = 0;
-    while ((1 << lg) < head_lanes(cache.head_dim)) ++lg;
-    int threads = lg;
-    while ((1 << threads) < kHeadThreads && (1 << (threads - lg)) < 2 * cache.n_kv) ++threads;
-    const int32_t groups = ((T_max - 1) >> (kHeadThreadsLog2 - threads)) + 1;
+    const TokenThreads n = token_threads(cache.head_dim, 2 * cache.n_kv, T_max);
     const auto kernel = bf16 ? (e4m3 ? kv_append_kernel<true, true> : kv_append_kernel<true, false>)
                              : (e4m3 ? kv_append_kernel<false, true> : kv_append_kernel<false, false>);
-    hipLaunchKernelGGL(kernel, token_grid(groups), dim3(kHeadThreads), 0, stream, k, k_stride, v,
-                       v_stride, lg, threads, T_max, req, pos, T_valid, rope, cache, err_word);
+    hipLaunchKernelGGL(kernel, n.grid, dim3(kHeadThreads), 0, stream, k, k_stride, v, v_stride,
+                       n.lanes_log2, n.threads_log2, T_max, req, pos, T_valid, rope, cache, err_word);
     return hipGetLastError();
 }
 
