@@ -163,3 +163,29 @@ def test_scaled_values_are_the_rounded_quotients(px, dtype):
         rows = got.view(torch.uint8).cpu().transpose(1, 2).reshape(T, n_kv, hd)
         assert torch.equal(rows, want)
     assert int(err.item()) == 0
+
+
+def test_more_workgroups_than_a_row_of_the_grid(px):
+    """Heads that take a workgroup a token, past 2^20 tokens."""
+    T, n, hd = 2 ** 20 + 3, 16, 256
+    x = torch.randn(1, n, hd, generator=torch.Generator().manual_seed(3)).to(BF).cuda()
+    q = x.expand(T, n, hd)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda") % 7
+    w = torch.ones(hd, dtype=BF, device="cuda")
+    few, out = torch.zeros(7, n, hd, dtype=BF, device="cuda"), torch.empty(T, n, hd, dtype=BF, device="cuda")
+    rope = px.Rope(1.0 / 10.0 ** torch.arange(hd // 2, dtype=torch.float64, device="cuda"))
+    px.xmix_qk_norm_rope(q[:7], None, pos[:7], w, None, 1e-6, rope, few, None)
+    px.xmix_qk_norm_rope(q, None, pos, w, None, 1e-6, rope, out, None)
+    whole = T // 7 * 7
+    assert bool((out[:whole].view(-1, 7, n, hd) == few).all()) and same(out[whole:], few[:T - whole])
+    cache = px.KvCache(*[torch.zeros(2, 8, 16, hd, dtype=BF, device="cuda") for _ in "kv"], i32([[0, 1]]))
+    req = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    req[[1, 2 ** 20, T - 1]] = 0
+    pos[[1, 2 ** 20, T - 1]] = i32([5, 6, 30])
+    err = i32([0])
+    px.xmix_kv_append(q[:, :8], q[:, 8:], req, pos, None, cache, err)
+    for got, want in ((cache.k, x[0, :8]), (cache.v, x[0, 8:])):
+        for page, slot in ((0, 5), (0, 6), (1, 14)):
+            assert same(got[page, :, slot], want)
+        assert int((got != 0).any(-1).sum()) == 3 * 8
+    assert int(err.item()) == 0
