@@ -58,9 +58,9 @@ __device__ __forceinline__ float head_sum(float v, int n) {
 // its key heads in turn, the next head's rows on their way while one is worked on; a
 // lane's angles are computed once for all of them.
 //   y = x (mean(x^2) + eps)^(-1/2) w,   out = round(rotate(y))
-// 8192 tokens of 64 + 8 heads of 128: 49.8 us for 302 MB, 6.1 TB/s (61.6 us with a
-// head loaded after the one before it was stored); 256 tokens of 32 + 8: 4.7 us,
-// launch and one round trip.
+// 8192 tokens of 64 + 8 heads of 128: 58 us for 302 MB, 5.2 TB/s, past a large copy's
+// 4.7, and 49.8 us where rows are still in the last cache (61.6 with a head loaded after
+// the one before it was stored); 256 tokens of 32 + 8: 4.7 us, launch and one round trip.
 template <bool BF16>
 __global__ void __launch_bounds__(kHeadThreads)
 norm_rope_kernel(HeadRows q, HeadRows k, int32_t head_dim, int32_t lanes_log2, int32_t threads_log2,
