@@ -265,10 +265,11 @@ class HookStep:
                 a = lay.attention
                 issue(f"L{li}/norm_rope", lambda a=a: xmix_qk_norm_rope(
                     a.q, None if a.k_rot is None else a.k, self.pos, a.q_weight, a.k_weight, a.eps,
-                    a.rope, a.q_rot, a.k_rot, stream=stream))
+                    a.rope, a.q_rot, a.k_rot, self.T_valid, stream=stream))
                 issue(f"L{li}/kv_append", lambda a=a: xmix_kv_append(
                     a.k if a.k_rot is None else a.k_rot, a.v, self.req, self.pos,
-                    a.rope if a.k_rot is None else None, a.cache, self.err, stream=stream))
+                    a.rope if a.k_rot is None else None, a.cache, self.err, self.T_valid,
+                    stream=stream))
                 issue(f"L{li}/attention", lambda a=a: xmix_paged_attention(
                     a.q_rot, self.cu, self.kv_len, a.cache, a.q.shape[2] ** -0.5, a.window,
                     self.max_q, a.out, None, self.err, self.attention_ws, stream=stream))
