@@ -1364,7 +1364,8 @@ attend_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
     if (threadIdx.x == 0) odd_unit = -1;
     __syncthreads();
     int unit = 0;
-    for (Span s{st.lo, st.n, st.len}; st.at < st.end; s = scalar_span(in, cache, st.req)) {
+    Span s{st.lo, st.n, st.len};
+    while (st.at < st.end) {
         const Blocks bl = blocks_of(s, st.tile, in.group, kRows, in.window);
         const int64_t begin = st.at + kDeal.extra;
         const int32_t step = few_rows(s.n, in.group) ? kDeal.few_step : kDeal.step, all = bl.count * step;
@@ -1381,15 +1382,14 @@ attend_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
         if (st.block + count < bl.count) break;
         st.at += kDeal.extra + all;
         st.block = 0;
-        if (NB || ++st.tile == tiles_of(s.n, in.group, kRows)) {
-            st.tile = 0;
-            if (++st.head == cache.n_kv) {
-                st.head = 0;
-                if (st.at < st.end)
-                    do ++st.req;
-                    while (st.req < cache.R_max - 1 && scalar_span(in, cache, st.req).n == 0);
-            }
-        }
+        if (!NB && ++st.tile < tiles_of(s.n, in.group, kRows)) continue;
+        st.tile = 0;
+        if (++st.head < cache.n_kv || st.at >= st.end) continue;
+        st.head = 0;
+        do {
+            ++st.req;
+            s = scalar_span(in, cache, st.req);
+        } while (st.req < cache.R_max - 1 && s.n == 0);
     }
 }
 
