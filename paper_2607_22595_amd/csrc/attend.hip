@@ -74,6 +74,7 @@ struct WorkRange {
     int32_t req, head, tile, block;  // the unit, and its block that is the first
     int32_t lo, n, len;              // the request's span and keys
     int32_t nth;                     // its place among the ranges
+    int32_t queued;                  // units of the launch in the queue
 };
 // What is dealt: a unit's place is `extra` for what it costs beside its blocks (its
 // queries, the first copies, its rows), then `step` for each block (`few_step` where
@@ -84,29 +85,41 @@ struct Deal {
     int32_t least;                  // places of a range, at least a step: no range between
                                     // the first and the last of a unit is without a block
     int32_t whole;                  // tiles of so many blocks are not cut
+    int32_t small;                  // leading tiles of so many blocks are not dealt but
+    int32_t queue_from;             // queued, in launches of so many places a workgroup
 };
 // A block of a tile takes half as long again as one of a row unit (1.4 us and 0.9 us
 // at head_dim 64, two workgroups on a CU), a unit's own cost is 6 to 8 us; sixteen
-// prompts take 145 us with 9 places for it, 150 with 12 and 148 with 15.  A launch of
+// prompts took 145 us with 9 places for it, 150 with 12 and 148 with 15.  A launch of
 // row units alone takes 643 us with 4 (256 requests of up to 8192 keys), 640 with 2,
 // 652 with 8; one request of 1024 keys 16.0, 18.7 and 16.1.
-constexpr Deal kDealRows = {0, 4, 1, 1, 4, 0}, kDealTiles = {kTileRows, 9, 3, 2, 3, 18};
+// Of a long launch of tiles the short units that lead each request (the first tokens of
+// a prompt) are left for whoever ends its range first: sixteen prompts 153 -> 142 us,
+// one of 2000 tokens 138 -> 119.  A short launch would pay for the queue's round trips
+// (one prompt of 40 tokens 15.5 -> 20.4), and row units in it leave the matrix units
+// idle at the end (95 single tokens and a chunk 128 -> 138).
+constexpr Deal kDealRows = {0, 4, 1, 1, 4, 0, 0, 0}, kDealTiles = {kTileRows, 9, 3, 2, 3, 18, 4, 32};
 __host__ __device__ constexpr Deal deal_of(int32_t rows) {
     Deal d = rows == kTileRows ? kDealTiles : kDealRows;
     d.rows = rows;
     return d;
 }
 // The workspace: a range per workgroup, a count of finished parts per range that
-// begins a cut unit, and two parts per range.
+// begins a cut unit, the queue, and two parts per range.  The queue: how many of its
+// units are taken; from kQueueHead on how many units there are up to each request
+// (R_max + 1 numbers); then each request's leading tiles that are in it (R_max).
 struct AttendWs {
     WorkRange* range;
     int32_t* done;
+    int32_t* queue;
     float* parts;
 };
+constexpr int kQueueHead = 4;
 template <>
 struct ArgPointers<AttendWs> {
     static std::vector<uint16_t> offsets() {
-        return {offsetof(AttendWs, range), offsetof(AttendWs, done), offsetof(AttendWs, parts)};
+        return {offsetof(AttendWs, range), offsetof(AttendWs, done), offsetof(AttendWs, queue),
+                offsetof(AttendWs, parts)};
     }
 };
 
@@ -196,13 +209,18 @@ __device__ __forceinline__ int64_t wave_sum64(int64_t v) {
 // the nearer end of it instead: its parts would take their way through memory, 64 KB
 // each, and sixteen prompts of 128 to 1024 tokens took 245 us with every end cut and
 // 211 so.
-template <bool MANY>
+template <bool MANY, bool TILES>
 __global__ void __launch_bounds__(kPlanThreads)
 attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t n_wg) {
     __shared__ Span spans[kMaxRequests];
     __shared__ int64_t upto[kMaxRequests + 1], begins[kMaxRanges + 1];
     __shared__ int64_t wave_total[kPlanThreads / kWave];
     __shared__ uint64_t tile_ranges[kMaxRanges / kWave];
+    constexpr int kQueued = TILES ? kMaxRequests : 0;
+    __shared__ int32_t queued[kQueued + 1];       // units in the queue up to a request
+    __shared__ int32_t wave_queued[kPlanThreads / kWave];
+    __shared__ uint8_t lead[kQueued + 1];         // a request's tiles in the queue, of each head,
+    __shared__ int32_t lead_places[kQueued + 1];  // and their places
     __shared__ uint16_t many[MANY ? kMaxRequests : 1];  // requests of many tiles
     __shared__ int n_many;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -210,9 +228,8 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t
     const HeadGroup group = in.group;
     const int32_t rows = deal.rows, extra = deal.extra;
     auto step_of = [&](int32_t n) { return few_rows(n, group) ? deal.few_step : deal.step; };
-    auto place_of = [&](const Span& s, int32_t t, int32_t step) {
-        return blocks_of(s, t, group, rows, in.window).count * step + extra;
-    };
+    auto count_of = [&](const Span& s, int32_t t) { return blocks_of(s, t, group, rows, in.window).count; };
+    auto small_of = [&](int32_t n) { return few_rows(n, group) ? 0 : deal.small; };
     if (MANY && tid == 0) n_many = 0;
     __syncthreads();
     bool bad = false;
@@ -224,9 +241,22 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t
             many[atomicAdd(&n_many, 1)] = static_cast<uint16_t>(r);
             continue;
         }
-        int64_t sum = 0;
-        for (int32_t t = 0; t < tiles; ++t) sum += place_of(s, t, step);
+        const int32_t small = small_of(s.n);
+        int64_t sum = 0, led = 0;
+        int32_t n = 0;
+        for (int32_t t = 0; t < tiles; ++t) {
+            const int32_t count = count_of(s, t), places = count * step + extra;
+            if (TILES && n == t && count <= small) {
+                ++n;
+                led += places;
+            }
+            sum += places;
+        }
         upto[r + 1] = sum * cache.n_kv;
+        if constexpr (TILES) {
+            lead[r] = static_cast<uint8_t>(n);
+            lead_places[r] = static_cast<int32_t>(led);
+        }
     }
     if constexpr (MANY) {
         __syncthreads();
@@ -234,35 +264,87 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t
             const int32_t r = many[i];
             const Span s = spans[r];
             const int32_t tiles = tiles_of(s.n, group, rows), step = step_of(s.n);
-            int64_t sum = 0;
-            for (int32_t t = lane; t < tiles; t += kWave) sum += place_of(s, t, step);
+            const uint64_t large = wave_ballot(lane >= tiles || count_of(s, lane) > small_of(s.n));
+            const int32_t n = large ? __builtin_ctzll(large) : kWave;
+            int64_t sum = 0, led = 0;
+            for (int32_t t = lane; t < tiles; t += kWave) {
+                const int32_t places = count_of(s, t) * step + extra;
+                sum += places;
+                if (t < n) led += places;
+            }
             sum = wave_sum64(sum);
-            if (lane == 0) upto[r + 1] = sum * cache.n_kv;
+            led = wave_sum64(led);
+            if (lane == 0) {
+                upto[r + 1] = sum * cache.n_kv;
+                lead[r] = static_cast<uint8_t>(n);
+                lead_places[r] = static_cast<int32_t>(led);
+            }
         }
     }
     if (bad && blockIdx.x == 0) atomicOr(in.err_word, kErrKvSpan);
-    if (tid == 0) upto[0] = 0;
+    if (tid == 0) upto[0] = queued[0] = 0;
     __syncthreads();
     // prefix over the requests, four to a thread
     constexpr int kEach = kMaxRequests / kPlanThreads;
+    if constexpr (TILES) {  // whether the launch is long enough for a queue
+        int64_t mine = 0;
+        for (int i = 0; i < kEach; ++i)
+            if (tid * kEach + i < R) mine += upto[tid * kEach + i + 1];
+        mine = wave_sum64(mine);
+        if (lane == 0) wave_total[wave] = mine;
+        __syncthreads();
+        int64_t all = 0;
+        for (int w = 0; w < kPlanThreads / kWave && w * kWave * kEach < R; ++w) all += wave_total[w];
+        const bool queue = all >= static_cast<int64_t>(deal.queue_from) * n_wg;
+        for (int i = 0; i < kEach; ++i) {
+            const int32_t r = tid * kEach + i;
+            if (r >= R) break;
+            if (queue) upto[r + 1] -= static_cast<int64_t>(lead_places[r]) * cache.n_kv;
+            else lead[r] = 0;
+        }
+        __syncthreads();
+    }
     int64_t v[kEach], sum = 0;
+    int32_t q[kEach], q_sum = 0;
     for (int i = 0; i < kEach; ++i) {
         const int32_t r = tid * kEach + i;
         sum += r < R ? upto[r + 1] : 0;
         v[i] = sum;
+        if constexpr (TILES) q_sum += r < R ? lead[r] * cache.n_kv : 0;
+        q[i] = q_sum;
     }
     int64_t incl = sum;
+    int32_t q_incl = q_sum;
     for (int o = 1; o < kWave; o <<= 1) {
         const int64_t up = __shfl_up(incl, o);
-        if (lane >= o) incl += up;
+        const int32_t q_up = TILES ? __shfl_up(q_incl, o) : 0;
+        if (lane >= o) {
+            incl += up;
+            q_incl += q_up;
+        }
     }
-    if (lane == kWave - 1) wave_total[wave] = incl;
+    if (lane == kWave - 1) {
+        wave_total[wave] = incl;
+        wave_queued[wave] = q_incl;
+    }
     __syncthreads();
     int64_t before = incl - sum;
-    for (int w = 0; w < wave; ++w) before += wave_total[w];
+    int32_t q_before = q_incl - q_sum;
+    for (int w = 0; w < wave && w * kWave * kEach < R; ++w) {
+        before += wave_total[w];
+        q_before += wave_queued[w];
+    }
     for (int i = 0; i < kEach; ++i)
-        if (tid * kEach + i < R) upto[tid * kEach + i + 1] = before + v[i];
+        if (tid * kEach + i < R) {
+            upto[tid * kEach + i + 1] = before + v[i];
+            if constexpr (TILES) queued[tid * kEach + i + 1] = q_before + q[i];
+        }
     __syncthreads();
+    if (TILES && blockIdx.x == 0) {
+        if (tid == 0) ws.queue[0] = 0;
+        for (int32_t r = tid; r <= R; r += kPlanThreads) ws.queue[kQueueHead + r] = queued[r];
+        for (int32_t r = tid; r < R; r += kPlanThreads) ws.queue[kQueueHead + R + 1 + r] = lead[r];
+    }
     const int64_t places = upto[R];
     const int64_t share = max(static_cast<int64_t>(deal.least), quotient(places + n_wg - 1, n_wg));
     // The last request that starts at or before a place.
@@ -281,14 +363,14 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t
         const Span s = spans[lo];
         const int64_t a_head = quotient(upto[lo + 1] - upto[lo], cache.n_kv), rest = at - upto[lo];
         const int32_t head = static_cast<int32_t>(quotient(rest, a_head));
-        WorkRange st{at, 0, share, lo, head, 0, 0, s.lo, s.n, s.len, 0};
+        WorkRange st{at, 0, share, lo, head, TILES ? lead[lo] : 0, 0, s.lo, s.n, s.len, 0, 0};
         int64_t left = rest - head * a_head;
         const int32_t tiles = tiles_of(s.n, group, rows), step = step_of(s.n);
         *count = 1;
         if constexpr (MANY) {  // 64 tiles at a time
             for (; st.tile < tiles; st.tile += kWave) {
                 const int32_t t = st.tile + lane;
-                const int32_t mine = t < tiles ? blocks_of(s, t, group, rows, in.window).count : 0;
+                const int32_t mine = t < tiles ? count_of(s, t) : 0;
                 int64_t incl = t < tiles ? mine * step + extra : 0;
                 for (int o = 1; o < kWave; o <<= 1) {
                     const int64_t up = __shfl_up(incl, o);
@@ -306,7 +388,7 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t
             }
         } else {
             for (; st.tile < tiles; ++st.tile) {
-                *count = blocks_of(s, st.tile, group, rows, in.window).count;
+                *count = count_of(s, st.tile);
                 if (left < *count * step + extra) break;
                 left -= *count * step + extra;
             }
@@ -316,7 +398,7 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t
         return st;
     };
     auto begin_of = [&](int32_t w) {
-        WorkRange st{places, 0, share, 0, 0, 0, 0, 0, 0, 0, 0};
+        WorkRange st{places, 0, share, 0, 0, 0, 0, 0, 0, 0, 0, 0};
         int32_t count;
         if (w * share < places) {
             st = locate(w * share, &count);
@@ -340,8 +422,7 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t
     // in their order and 161 with the rows first.
     const int32_t used = static_cast<int32_t>(min(static_cast<int64_t>(n_wg), quotient(places + share - 1, share)));
     const int32_t each = (used + 7) / 8;
-    const bool mixed = deal.step != deal.few_step;
-    if (mixed) {
+    if constexpr (TILES) {
         if (tid < kMaxRanges) {
             bool tile = false;
             if (tid < used) {
@@ -355,7 +436,7 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t
     }
     auto workgroup_of = [&](int32_t w) {
         if (w >= 8 * each) return w;
-        if (!mixed) return w / each + 8 * (w % each);
+        if (!TILES) return w / each + 8 * (w % each);
         int32_t before = 0, all = 0;  // ranges of tiles
         for (int32_t i = 0; i < kMaxRanges / kWave; ++i) {
             const uint64_t mask = tile_ranges[i];
@@ -383,6 +464,7 @@ attend_plan_kernel(AttendIn in, KvCacheIn cache, AttendWs ws, Deal deal, int32_t
         st.end = begins[i + 1];
         if (begins[i] == st.end) st.end = st.at;  // nothing to do
         st.nth = w;
+        st.queued = TILES ? queued[R] : 0;
         ws.range[workgroup_of(w)] = st;
     };
     if constexpr (MANY) {  // a wave a range
@@ -708,7 +790,7 @@ __device__ __forceinline__ WorkRange range_of(const AttendWs& ws) {
     const WorkRange* r = ws.range + blockIdx.x;
     return {scalar_load(&r->at), scalar_load(&r->end), scalar_load(&r->share), scalar_load(&r->req),
             scalar_load(&r->head), scalar_load(&r->tile), scalar_load(&r->block), scalar_load(&r->lo),
-            scalar_load(&r->n), scalar_load(&r->len), scalar_load(&r->nth)};
+            scalar_load(&r->n), scalar_load(&r->len), scalar_load(&r->nth), scalar_load(&r->queued)};
 }
 
 // ------------------------------------------------------------------ tile units
@@ -1357,19 +1439,45 @@ attend_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
     __shared__ OddKeys odd_keys[kAttendWaves * HD];
     __shared__ uint32_t notes[2 * kRows * HD / 32];
     __shared__ float wm[kAttendWaves * (NB ? kRows : kFewRows)], wl[kAttendWaves * (NB ? kRows : kFewRows)];
-    __shared__ int flag, odd_unit;
+    __shared__ int flag, odd_unit, taken;
     const UnitLds lds{a, b, odd_keys, notes, wm, wl, &flag, &odd_unit};
     WorkRange st = range_of(ws);
-    if (st.at >= st.end) return;
+    if (st.at >= st.end && !(NB == 0 && st.queued)) return;
     if (threadIdx.x == 0) odd_unit = -1;
     __syncthreads();
-    int unit = 0;
+    // The range first, then units of the queue: whole and short ones, which even out
+    // when the workgroups end; who takes one makes no difference to its result.
     Span s{st.lo, st.n, st.len};
-    while (st.at < st.end) {
+    for (int unit = 0;; ++unit) {
+        const bool dealt = st.at < st.end;
+        if (!dealt) {
+            if constexpr (NB) break;
+            if (!st.queued) break;
+            if (threadIdx.x == 0)
+                taken = __hip_atomic_fetch_add(ws.queue, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __syncthreads();  // (a unit has barriers, so the one before has been read)
+            const int32_t nth = scalar(taken);
+            if (nth >= st.queued) break;
+            const int32_t* upto = ws.queue + kQueueHead;
+            int32_t lo = 0, hi = cache.R_max - 1;  // the last request that starts at or before nth
+            while (lo < hi) {
+                const int32_t mid = (lo + hi + 1) >> 1;
+                if (scalar_load(upto + mid) <= nth) lo = mid;
+                else hi = mid - 1;
+            }
+            const int32_t rest = nth - scalar_load(upto + lo);
+            const int32_t lead = scalar_load(upto + cache.R_max + 1 + lo);
+            s = scalar_span(in, cache, lo);
+            st.req = lo;
+            st.head = scalar(static_cast<int32_t>(static_cast<uint32_t>(rest) / static_cast<uint32_t>(max(lead, 1))));
+            st.tile = rest - st.head * lead;
+            st.block = 0;
+        }
         const Blocks bl = blocks_of(s, st.tile, in.group, kRows, in.window);
         const int64_t begin = st.at + kDeal.extra;
         const int32_t step = few_rows(s.n, in.group) ? kDeal.few_step : kDeal.step, all = bl.count * step;
-        const int32_t count = static_cast<int32_t>(min(st.end - begin, static_cast<int64_t>(all))) / step - st.block;
+        const int32_t count =
+            dealt ? static_cast<int32_t>(min(st.end - begin, static_cast<int64_t>(all))) / step - st.block : bl.count;
         if constexpr (NB) {
             row_unit<HD, E4M3, NB, kRows>(in, cache, ws, st, s, bl, begin, begin + all - step, count, unit, lds);
         } else {
@@ -1378,18 +1486,22 @@ attend_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
             else
                 tile_unit<HD, E4M3>(in, cache, ws, st, s, bl, begin, begin + all - step, count, unit, lds);
         }
-        ++unit;
-        if (st.block + count < bl.count) break;
+        if (!dealt) continue;
+        if (st.block + count < bl.count) {
+            st.at = st.end;
+            continue;
+        }
         st.at += kDeal.extra + all;
         st.block = 0;
         if (!NB && ++st.tile < tiles_of(s.n, in.group, kRows)) continue;
-        st.tile = 0;
+        st.tile = NB ? 0 : scalar_load(ws.queue + kQueueHead + cache.R_max + 1 + st.req);
         if (++st.head < cache.n_kv || st.at >= st.end) continue;
         st.head = 0;
         do {
             ++st.req;
             s = scalar_span(in, cache, st.req);
-        } while (st.req < cache.R_max - 1 && s.n == 0);
+            if (!NB) st.tile = scalar_load(ws.queue + kQueueHead + cache.R_max + 1 + st.req);
+        } while (st.req < cache.R_max - 1 && (s.n == 0 || (!NB && st.tile >= tiles_of(s.n, in.group, kRows))));
     }
 }
 
@@ -1412,13 +1524,15 @@ int32_t workgroups(int32_t rows, const KvCacheIn& c) {
 }
 
 struct WsLayout {
-    size_t done, parts, bytes;
+    size_t done, queue, parts, bytes;
 };
 WsLayout ws_layout(int32_t rows, const KvCacheIn& c) {
     const size_t n = static_cast<size_t>(workgroups(rows, c));
     WsLayout w;
     w.done = n * sizeof(WorkRange);
-    w.parts = w.done + n * sizeof(int32_t);
+    w.queue = w.done + n * sizeof(int32_t);
+    w.parts = w.queue;
+    if (rows == kTileRows) w.parts += (kQueueHead + 2 * static_cast<size_t>(c.R_max) + 1 + 3) / 4 * 16;
     w.bytes = w.parts + 2 * n * rows * static_cast<size_t>(c.head_dim + 2) * sizeof(float);
     return w;
 }
@@ -1448,14 +1562,13 @@ hipError_t launch_attend(const AttendIn& in, const KvCacheIn& cache, bool e4m3, 
     const WsLayout w = ws_layout(rows, cache);
     char* p = static_cast<char*>(ws);
     const AttendWs aw{reinterpret_cast<WorkRange*>(p), reinterpret_cast<int32_t*>(p + w.done),
-                      reinterpret_cast<float*>(p + w.parts)};
+                      reinterpret_cast<int32_t*>(p + w.queue), reinterpret_cast<float*>(p + w.parts)};
     const int64_t most = (static_cast<int64_t>(in.max_q) * (in.n_q / cache.n_kv) + rows - 1) / rows;
-    if (most > kTilesEach)
-        hipLaunchKernelGGL(attend_plan_kernel<true>, dim3(n_wg / kPlanRanges), dim3(kPlanThreads), 0,
-                           stream, in, cache, aw, deal_of(rows), n_wg);
-    else
-        hipLaunchKernelGGL(attend_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, stream, in, cache, aw,
-                           deal_of(rows), n_wg);
+    const auto plan = rows != kTileRows     ? attend_plan_kernel<false, false>
+                      : most <= kTilesEach ? attend_plan_kernel<false, true>
+                                           : attend_plan_kernel<true, true>;
+    hipLaunchKernelGGL(plan, dim3(most <= kTilesEach ? 1 : n_wg / kPlanRanges), dim3(kPlanThreads), 0, stream, in,
+                       cache, aw, deal_of(rows), n_wg);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel_for(cache.head_dim, e4m3, rows), dim3(n_wg), dim3(kAttendThreads), 0, stream,
@@ -1464,8 +1577,9 @@ hipError_t launch_attend(const AttendIn& in, const KvCacheIn& cache, bool e4m3, 
 }
 
 void add_attend_kernels(std::vector<KernelInfo>& t) {
-    t.push_back(kernel_info(attend_plan_kernel<false>));
-    t.push_back(kernel_info(attend_plan_kernel<true>));
+    t.push_back(kernel_info(attend_plan_kernel<false, false>));
+    t.push_back(kernel_info(attend_plan_kernel<false, true>));
+    t.push_back(kernel_info(attend_plan_kernel<true, true>));
     for (const auto& width : kKernels)
         for (const auto& type : width)
             for (const AttendKernel k : type)
