@@ -18,7 +18,8 @@
 // they cost, are cut into equal ranges, one per workgroup, whatever the lengths are.
 // A unit that is cut leaves a part (maximum, sum, O) per workgroup in the workspace,
 // and the last workgroup to finish one joins them in order.  attend_plan_kernel finds
-// where each range starts.
+// where each range starts.  Short tiles of a long launch are taken from a queue at the
+// ends of the ranges, each as a whole.
 //
 // Two kinds of unit, each with an inner loop of its own:
 //   tile unit   128 rows; the workgroup's four waves take 32 rows each and share K
@@ -813,7 +814,7 @@ struct UnitLds {
 // heads of 128, run at 930 to 990 TFLOP/s (2.1 to 2.2 ms; 53 % of the cycles in matrix
 // instructions, the library's plain product reaches 1249).  With few blocks a unit
 // its start does, the chain from page id to copy to first product: units of one block
-// take 9 us, of eight 18 (sixteen prompts of up to 1024 tokens: 145 us, 470 TFLOP/s).
+// take 9 us, of eight 18 (sixteen prompts of up to 1024 tokens: 143 us, 485 TFLOP/s).
 // The next unit's first copies issued before this one's rows are stored did not help
 // (147 to 159 us), the CU's second workgroup being at work meanwhile.
 template <int HD, bool E4M3>
