@@ -1474,6 +1474,7 @@ attend_kernel(AttendIn in, KvCacheIn cache, AttendWs ws) {
             st.tile = rest - st.head * lead;
             st.block = 0;
         }
+        if (st.tile >= tiles_of(s.n, in.group, kRows)) break;  // (lengths changed under the call)
         const Blocks bl = blocks_of(s, st.tile, in.group, kRows, in.window);
         const int64_t begin = st.at + kDeal.extra;
         const int32_t step = few_rows(s.n, in.group) ? kDeal.few_step : kDeal.step, all = bl.count * step;
