@@ -680,7 +680,8 @@ xmix_status xmix_kv_append(const void *k, int64_t k_stride, const void *v, int64
  * is longer.  A span outside [0, T_max] or longer than max_q, or a key count
  * outside [0, max_pages * page_size] of a request with tokens, sets
  * XMIX_ERR_KV_SPAN and the request's rows are not written.  A page id outside
- * [0, n_pages) sets XMIX_ERR_KV_PAGE and its keys are left out.
+ * [0, n_pages) with a key that some token sees sets XMIX_ERR_KV_PAGE and its keys
+ * are left out; entries of pages wholly behind the window may hold anything.
  * Requires head_dim 64, 128 or 256, n_q % n_kv == 0, scale > 0 and finite,
  * window >= 0, 1 <= max_q, R_max <= 4096.
  * ws: 16-byte aligned device workspace of xmix_paged_attention_workspace

@@ -543,6 +543,17 @@ __device__ __forceinline__ uint32_t groups_gone(const KvCacheIn& c, int32_t ids,
     return static_cast<uint32_t>(wave_ballot(!page_ok(c, ids))) & ((1u << groups) - 1);
 }
 
+// Whether a missing group (`gone`, of the block from key0 on) has a key that rows at the
+// positions p_first to p_last see.  A block begins at a multiple of its keys: the pages
+// wholly behind a window may have been given away.
+__device__ __forceinline__ bool gone_seen(uint32_t gone, int32_t key0, int32_t p_first, int32_t p_last,
+                                          int32_t window) {
+    if (p_last < key0) return false;
+    const int32_t from = window > 0 && p_first >= window ? p_first - window + 1 : 0;
+    const int32_t a = max(from - key0, 0) / kGroupKeys, b = min(p_last - key0, kBlockKeys - 1) / kGroupKeys;
+    return a <= b && (gone & ((2u << b) - (1u << a))) != 0;
+}
+
 // An offset that the compiler computes from here on anew: a tile's reads differ by an
 // exclusive or with a constant (the permutation of the pieces), one instruction each,
 // and kept apart would hold a register each through the whole loop.
@@ -937,7 +948,8 @@ __device__ __forceinline__ void tile_unit(const AttendIn& in, const KvCacheIn& c
         }
         if (gone || key0 + kBlockKeys - 1 > p_first ||
             (in.window > 0 && key0 <= p_last - in.window)) {
-            if (gone && lane == 0 && key0 < s.len) atomicOr(in.err_word, kErrKvPage);
+            if (gone && lane == 0 && gone_seen(gone, key0, p_first, p_last, in.window))
+                atomicOr(in.err_word, kErrKvPage);
             const int32_t from = in.window > 0 ? pos - in.window : -1;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
@@ -1246,7 +1258,8 @@ __device__ __forceinline__ void row_unit(const AttendIn& in, const KvCacheIn& ca
             }
         }
         if (gone || key0 + KS - 1 > p_first || (in.window > 0 && key0 <= p_last - in.window)) {
-            if (gone && lane == 0 && key0 < s.len) atomicOr(in.err_word, kErrKvPage);
+            if (gone && lane == 0 && gone_seen(gone, key0, p_first, p_last, in.window))
+                atomicOr(in.err_word, kErrKvPage);
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 const int32_t from = in.window > 0 ? pos[b] - in.window : -1;
