@@ -696,6 +696,17 @@ xmix_status xmix_paged_attention(const uint16_t *q, int64_t q_stride, int32_t n_
                                  const xmix_kv_cache *cache, float scale, int32_t window,
                                  int32_t max_q, uint16_t *out, int64_t out_stride, float *lse_out,
                                  uint32_t *err_word, void *ws, size_t ws_bytes, void *stream);
+/* The same, of the tokens below *T_valid [1] int32, device (NULL: all): those of a span
+ * that runs past it keep their positions, kv_len being the whole span's; the rows at or
+ * past it are neither read nor written, nor are their keys and values.  A negative
+ * count is none, one past T_max all. */
+xmix_status xmix_paged_attention_valid(const uint16_t *q, int64_t q_stride, int32_t n_q,
+                                       int32_t T_max, const int32_t *cu_seqlens,
+                                       const int32_t *kv_len, const xmix_kv_cache *cache,
+                                       float scale, int32_t window, int32_t max_q, uint16_t *out,
+                                       int64_t out_stride, float *lse_out, uint32_t *err_word,
+                                       void *ws, size_t ws_bytes, const int32_t *T_valid,
+                                       void *stream);
 
 /* ------------------------------------------------------------ step graphs
  * A hook step captured once and replayed, with the kernel-node parameter

@@ -148,6 +148,9 @@ _sigs = {
     "xmix_paged_attention_workspace": ([_i32, _i32, _i32, ctypes.POINTER(XmixKvCache)], _sz),
     "xmix_paged_attention": ([_vp, _i64, _i32, _i32, _vp, _vp, ctypes.POINTER(XmixKvCache), _f32,
                               _i32, _i32, _vp, _i64, _vp, _vp, _vp, _sz, _vp], _st),
+    "xmix_paged_attention_valid": ([_vp, _i64, _i32, _i32, _vp, _vp, ctypes.POINTER(XmixKvCache),
+                                    _f32, _i32, _i32, _vp, _i64, _vp, _vp, _vp, _sz, _vp, _vp],
+                                   _st),
     "xmix_readback_compact": ([_vp, _vp, _i32, ctypes.POINTER(XmixRoute), _i32, _vp, _i32, _i32,
                                ctypes.POINTER(XmixRing), _vp], _st),
 }
@@ -226,10 +229,10 @@ _kv_append = _native(
     "D:dim err?:i32 T_valid?:i32 stream:here",
     "k /k v /v @A T req pos rope cache err T_valid stream")
 _paged_attention = _native(
-    "xmix_paged_attention",
+    "xmix_paged_attention_valid",
     "q:bf16~[T,n,D] cu:i32 kv_len:i32[R] cache:struct(Cache) R:dim D:dim scale:float window:int "
-    "max_q:int out:bf16~[T,n,D] lse?:f32[n,T] err?:i32 ws?:* stream:here",
-    "q /q n T cu kv_len cache scale window max_q out /out lse err ws %ws stream")
+    "max_q:int out:bf16~[T,n,D] lse?:f32[n,T] err?:i32 ws?:* T_valid?:i32 stream:here",
+    "q /q n T cu kv_len cache scale window max_q out /out lse err ws %ws T_valid stream")
 _graph_launch = _native("xmix_graph_launch", "graph:int stream:stream", "graph stream")
 
 
@@ -747,14 +750,16 @@ def paged_attention_workspace(T_max: int, n_q: int, max_q: int, cache: KvCache) 
 
 
 def xmix_paged_attention(q, cu_seqlens, kv_len, cache: KvCache, scale: float, window: int,
-                         max_q: int, out, lse_out, err_word, ws, stream=None):
+                         max_q: int, out, lse_out, err_word, ws, stream=None, T_valid=None):
     """Attention of the tokens q [T_max, n_q, head_dim] bf16 over the pages of
     their requests into out (the same shape; lse_out fp32 [n_q, T_max] or None).
     cu_seqlens int32 [R_max + 1], kv_len int32 [R_max] (cached keys, the step's own
     among them); window: the keys a token sees at most, itself among them (0: all);
-    max_q: no span is longer; ws: uint8, paged_attention_workspace bytes."""
+    max_q: no span is longer; ws: uint8, paged_attention_workspace bytes; T_valid
+    int32 [1]: rows at or past it are left out (a span that it cuts keeps the
+    positions of its tokens)."""
     assert cu_seqlens.numel() == cache.R_max + 1
     _beside(q, cache)
     _check("xmix_paged_attention", _paged_attention(
         q, cu_seqlens, kv_len, cache, cache.R_max, cache.head_dim, scale, window, max_q, out,
-        lse_out, err_word, ws, stream))
+        lse_out, err_word, ws, T_valid, stream))

@@ -688,11 +688,12 @@ size_t xmix_paged_attention_workspace(int32_t T_max, int32_t n_q, int32_t max_q,
     return attend_workspace(n_q, max_q, c);
 }
 
-xmix_status xmix_paged_attention(const uint16_t* q, int64_t q_stride, int32_t n_q, int32_t T_max,
-                                 const int32_t* cu_seqlens, const int32_t* kv_len,
-                                 const xmix_kv_cache* cache, float scale, int32_t window,
-                                 int32_t max_q, uint16_t* out, int64_t out_stride, float* lse_out,
-                                 uint32_t* err_word, void* ws, size_t ws_bytes, void* stream) {
+xmix_status xmix_paged_attention_valid(const uint16_t* q, int64_t q_stride, int32_t n_q, int32_t T_max,
+                                       const int32_t* cu_seqlens, const int32_t* kv_len,
+                                       const xmix_kv_cache* cache, float scale, int32_t window,
+                                       int32_t max_q, uint16_t* out, int64_t out_stride,
+                                       float* lse_out, uint32_t* err_word, void* ws,
+                                       size_t ws_bytes, const int32_t* T_valid, void* stream) {
     KvCacheIn c;
     if (!cache_ok(cache, &c) || T_max < 1 || !cu_seqlens || !kv_len || !err_word || window < 0 ||
         !(scale > 0.0f) || scale > 3.4e38f || !attend_heads_ok(n_q, max_q, c) ||
@@ -711,6 +712,7 @@ xmix_status xmix_paged_attention(const uint16_t* q, int64_t q_stride, int32_t n_
     in.out_stride = out_stride;
     in.lse = lse_out;
     in.err_word = err_word;
+    in.T_valid = T_valid;
     in.n_q = n_q;
     in.T_max = T_max;
     in.window = window;
@@ -722,6 +724,16 @@ xmix_status xmix_paged_attention(const uint16_t* q, int64_t q_stride, int32_t n_
                        ? static_cast<uint32_t>((int64_t{1} << 32) / n + 1)
                        : 0;
     return launched(launch_attend(in, c, cache->dt == XMIX_E4M3, ws, as_stream(stream)));
+}
+
+xmix_status xmix_paged_attention(const uint16_t* q, int64_t q_stride, int32_t n_q, int32_t T_max,
+                                 const int32_t* cu_seqlens, const int32_t* kv_len,
+                                 const xmix_kv_cache* cache, float scale, int32_t window,
+                                 int32_t max_q, uint16_t* out, int64_t out_stride, float* lse_out,
+                                 uint32_t* err_word, void* ws, size_t ws_bytes, void* stream) {
+    return xmix_paged_attention_valid(q, q_stride, n_q, T_max, cu_seqlens, kv_len, cache, scale,
+                                      window, max_q, out, out_stride, lse_out, err_word, ws,
+                                      ws_bytes, nullptr, stream);
 }
 
 }  // extern "C"

@@ -39,7 +39,8 @@ template <>
 struct ArgPointers<AttendIn> {
     static std::vector<uint16_t> offsets() {
         return {offsetof(AttendIn, q), offsetof(AttendIn, cu), offsetof(AttendIn, kv_len),
-                offsetof(AttendIn, out), offsetof(AttendIn, lse), offsetof(AttendIn, err_word)};
+                offsetof(AttendIn, out), offsetof(AttendIn, lse), offsetof(AttendIn, err_word),
+                offsetof(AttendIn, T_valid)};
     }
 };
 
@@ -141,7 +142,9 @@ __device__ __forceinline__ T scalar_load(const T* p) {
     return *(const __attribute__((address_space(4))) T*)reinterpret_cast<uintptr_t>(p);
 }
 
-// A request's span and keys; n = 0 where it has no rows to write.
+// A request's span and keys; n = 0 where it has no rows to write.  Of a span that runs
+// past the valid tokens the ones before stay, at their positions (len is then the key
+// count up to the last of them, and negative where none of them has a key).
 struct Span {
     int32_t lo, n, len;
 };
@@ -157,7 +160,10 @@ __device__ __forceinline__ Span span_of(const AttendIn& in, const KvCacheIn& c, 
         if (bad) *bad = true;
         return s;
     }
-    s.n = hi - lo;
+    const int32_t end = in.T_valid ? min(hi, scalar_load(in.T_valid)) : hi;
+    if (end <= lo) return s;
+    s.n = end - lo;
+    s.len = len - (hi - end);
     return s;
 }
 __device__ __forceinline__ Span span_of(const AttendIn& in, const KvCacheIn& c, int32_t r, bool* bad = nullptr) {

@@ -222,6 +222,7 @@ struct AttendIn {
     int64_t out_stride;
     float* lse;  // may be NULL
     uint32_t* err_word;
+    const int32_t* T_valid;  // may be NULL
     int32_t n_q, T_max, window, max_q;
     float scale;
     HeadGroup group;

@@ -272,7 +272,8 @@ class HookStep:
                     stream=stream))
                 issue(f"L{li}/attention", lambda a=a: xmix_paged_attention(
                     a.q_rot, self.cu, self.kv_len, a.cache, a.q.shape[2] ** -0.5, a.window,
-                    self.max_q, a.out, None, self.err, self.attention_ws, stream=stream))
+                    self.max_q, a.out, None, self.err, self.attention_ws, stream=stream,
+                    T_valid=self.T_valid))
             fused = None  # the token probes that run in one pass with the steering
             if self.fuse_steer_probe and lay.steer_v is not None:
                 fused = next((p for p in lay.probes if p.mode == XMIX_PROBE_TOKEN), None)
