@@ -230,7 +230,7 @@ _kv_append = _native(
     "k /k v /v @A T req pos rope cache err T_valid stream")
 _paged_attention = _native(
     "xmix_paged_attention_valid",
-    "q:bf16~[T,n,D] cu:i32 kv_len:i32[R] cache:struct(Cache) R:dim D:dim scale:float window:int "
+    "q:bf16~[T,n,D] cu:i32{C} kv_len:i32[R] cache:struct(Cache) R:dim C:dim D:dim scale:float window:int "
     "max_q:int out:bf16~[T,n,D] lse?:f32[n,T] err?:i32 ws?:* T_valid?:i32 stream:here",
     "q /q n T cu kv_len cache scale window max_q out /out lse err ws %ws T_valid stream")
 _graph_launch = _native("xmix_graph_launch", "graph:int stream:stream", "graph stream")
@@ -758,8 +758,7 @@ def xmix_paged_attention(q, cu_seqlens, kv_len, cache: KvCache, scale: float, wi
     max_q: no span is longer; ws: uint8, paged_attention_workspace bytes; T_valid
     int32 [1]: rows at or past it are left out (a span that it cuts keeps the
     positions of its tokens)."""
-    assert cu_seqlens.numel() == cache.R_max + 1
     _beside(q, cache)
     _check("xmix_paged_attention", _paged_attention(
-        q, cu_seqlens, kv_len, cache, cache.R_max, cache.head_dim, scale, window, max_q, out,
+        q, cu_seqlens, kv_len, cache, cache.R_max, cache.R_max + 1, cache.head_dim, scale, window, max_q, out,
         lse_out, err_word, ws, T_valid, stream))
