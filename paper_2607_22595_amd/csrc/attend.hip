@@ -192,7 +192,7 @@ __device__ __forceinline__ Blocks blocks_of(const Span& s, int32_t t, const Head
     const int32_t hi = s.len - s.n + tok1 + 1, p0 = s.len - s.n + tok0;
     const int32_t lo = window > 0 && p0 >= window ? p0 - window + 1 : 0;
     const int32_t first = hi > 0 ? lo / kBlockKeys : 0;
-    const int32_t end = hi > 0 ? (hi + kBlockKeys - 1) / kBlockKeys : 1;
+    const int32_t end = hi > 0 ? (hi - 1) / kBlockKeys + 1 : 1;  // (hi may be next to 2^31)
     return {first, end - first};
 }
 
@@ -538,10 +538,11 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t group_rows(const void* base, c
 // the request's last key, that one's).  They are loaded a step before they are needed,
 // by a vector load, which completes in order with the copies around it; a scalar load
 // would make every wait for LDS one for everything.
-__device__ __forceinline__ int32_t page_ids(const KvCacheIn& c, int32_t req, int32_t key0, int32_t len,
+// A key0 past the last one may be past 2^31 too.
+__device__ __forceinline__ int32_t page_ids(const KvCacheIn& c, int32_t req, uint32_t key0, int32_t len,
                                             int groups) {
-    const int32_t key = key0 + (lane_id() & (groups - 1)) * kGroupKeys;
-    const int32_t nth = max(0, min(key, len - 1)) >> c.page_log2;
+    const uint32_t key = key0 + (lane_id() & (groups - 1)) * kGroupKeys;
+    const uint32_t nth = min(key, static_cast<uint32_t>(max(0, len - 1))) >> c.page_log2;
     return (c.pages + static_cast<int64_t>(req) * c.max_pages)[nth];
 }
 // The groups whose page is not there, as bits.
@@ -890,7 +891,7 @@ __device__ __forceinline__ void tile_unit(const AttendIn& in, const KvCacheIn& c
     int32_t ids;        // of the block to be copied next
     uint32_t gone = 0;  // of the block whose turn it is
     auto load_ids = [&](int32_t block) __attribute__((always_inline)) {
-        ids = page_ids(cache, st.req, block * kBlockKeys, s.len, kGroups);
+        ids = page_ids(cache, st.req, static_cast<uint32_t>(block) * kBlockKeys, s.len, kGroups);
     };
     // Copies a block and asks for the ids of the one after it.
     auto stage = [&](int32_t block, uint4* kd, uint4* vd) __attribute__((always_inline)) {
@@ -1193,11 +1194,13 @@ __device__ __forceinline__ void row_unit(const AttendIn& in, const KvCacheIn& ca
     // K would be for everything outstanding.
     int32_t ids;  // page ids of the step whose loads come next
     auto load_ids = [&](int32_t step) __attribute__((always_inline)) {
-        ids = page_ids(cache, st.req, key_from + step * KS, s.len, kGroups);
+        ids = page_ids(cache, st.req, static_cast<uint32_t>(key_from) + static_cast<uint32_t>(step) * KS, s.len,
+                       kGroups);
     };
     auto stage = [&](int32_t step, uint4 (&K)[kGroups][kLoads], uint4* vd, uint32_t& gone)
         __attribute__((always_inline)) {
-        const int32_t key0 = key_from + step * KS, len = step < steps ? s.len : 0;
+        const bool on = step < steps;
+        const int32_t key0 = on ? key_from + step * KS : 0, len = on ? s.len : 0;
         __amdgpu_buffer_rsrc_t vr[kGroups];
         int32_t page[kGroups];
         gone = groups_gone(cache, ids, kGroups);

@@ -1,9 +1,10 @@
 """Sizes of the attention's arguments: what is shorter than the kernels read is refused
-before a launch, by the binding itself."""
+before a launch, by the binding itself; key counts up to the last one below 2^31."""
+import numpy as np
 import pytest
 import torch
 
-from test_gpu_attend import batch, i32, word
+from test_gpu_attend import BF, E4, attend, batch, check_attention, i32, reference, word
 
 pytestmark = pytest.mark.gpu
 
@@ -27,3 +28,27 @@ def test_span_starts_of_another_length(px, short):
         px._paged_attention(b["q"], cu, i32(b["kv_len"]), b["cache"], 3, 4, 64, 0.1, 0, 2, out, None, word(), ws,
                             None, None)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("stored", [BF, E4])
+@pytest.mark.parametrize("n,hd,n_q,n_kv", [(1, 128, 4, 1), (5, 64, 8, 2), (200, 128, 4, 1), (200, 64, 8, 2), (3, 256, 2, 1)])
+def test_key_counts_next_to_two_to_the_31(px, n, hd, n_q, n_kv, stored):
+    """The last keys that a table of pages of 16 can hold, in a window: the same as those
+    of a short request with the same last pages."""
+    last, window = 80, 1000
+    b = dict(batch(px, 61, [n], [last * 16], n_q, n_kv, hd, 16, stored), window=window)
+    ref = reference(b)
+    c = b["cache"]
+    max_pages = 2 ** 27 - 1
+    table = torch.full((1, max_pages), -1, dtype=torch.int32, device="cuda")
+    table[:, -last:] = c.pages
+    far = px.KvCache(c.k, c.v, table, c.k_scale, c.v_scale)
+    got = attend(px, dict(b, cache=far, kv_len=np.array([max_pages * 16])))
+    assert got[2] == 0
+    check_attention(got, ref, hd)
+    x = torch.randn(1, n_kv, hd, device="cuda").to(BF)
+    err, pos = word(), max_pages * 16 - 1
+    px.xmix_kv_append(x, x, i32([0]), i32([pos]), None, far, err)
+    at = int(table[0, -1])
+    scale = 1.0 if c.v_scale is None else c.v_scale[:, None]
+    assert torch.equal(c.v[at, :, 15].float(), (x[0].float() / scale).to(stored).float()) and err.item() == 0
