@@ -606,6 +606,13 @@ __device__ __forceinline__ bf16x8_t e4m3_to_bf16(int lo, int hi) {
     w.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
     return as_bf16x8(w);
 }
+// What a product q . k is multiplied by, for powers of two.  Where it leaves fp32's range
+// it is the least or the largest number there: zero would make NaN of a masked score
+// (-inf), an infinity of a product of zero.
+__device__ __forceinline__ float score_scale(float scale, float k_scale) {
+    const float c = scale * k_scale * kLog2e;
+    return c == 0.0f ? 0x1p-149f : c == INFINITY ? 0x1.fffffep127f : c;
+}
 // Weights to bf16, nearest even: 2^-9 of each on average, which the sum over many
 // keys averages out; the sum of the weights keeps them in fp32.
 __device__ __forceinline__ uint32_t weights2(float a, float b) {
@@ -864,7 +871,7 @@ __device__ __forceinline__ void tile_unit(const AttendIn& in, const KvCacheIn& c
     const int v_piece = E4M3 ? side : 2 * side + ((i16 & 3) >> 1);
     const int v_off = v_row * RB + ((v_piece ^ swz_v_tile<RB, E4M3>(v_row)) * 16) + 8 * (i16 & 1);
     const RowsOut u{s.lo, s.n * group.n, st.tile * kTileRows, st.head, group};
-    const float c2 = in.scale * (E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f) * kLog2e;
+    const float c2 = score_scale(in.scale, E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f);
     const float v_scale = E4M3 ? scalar_load(cache.v_scale + st.head) : 1.0f;
     // this lane's row, and the tokens of the wave's rows
     const int32_t row = u.row0 + wave * 32 + n32;
@@ -1166,7 +1173,7 @@ __device__ __forceinline__ void row_unit(const AttendIn& in, const KvCacheIn& ca
     const int v_off = wave * kTile * 16 + v_row * RB + ((v_piece ^ swz_v_row<RB, E4M3>(v_row)) * 16) +
                       8 * (n16 & 1);
     const RowsOut u{s.lo, s.n * group.n, 0, st.head, group};
-    const float c2 = in.scale * (E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f) * kLog2e;
+    const float c2 = score_scale(in.scale, E4M3 ? scalar_load(cache.k_scale + st.head) : 1.0f);
     const int32_t base = s.len - s.n;
     const int32_t p_first = base, p_last = s.len - 1;
     int32_t pos[NB];

@@ -1,10 +1,11 @@
 """Sizes of the attention's arguments: what is shorter than the kernels read is refused
-before a launch, by the binding itself; key counts up to the last one below 2^31."""
+before a launch, by the binding itself; key counts up to the last one below 2^31, and
+scales at the ends of fp32."""
 import numpy as np
 import pytest
 import torch
 
-from test_gpu_attend import BF, E4, attend, batch, check_attention, i32, reference, word
+from test_gpu_attend import BF, E4, SPANS, attend, batch, check_attention, i32, reference, word
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +53,20 @@ def test_key_counts_next_to_two_to_the_31(px, n, hd, n_q, n_kv, stored):
     at = int(table[0, -1])
     scale = 1.0 if c.v_scale is None else c.v_scale[:, None]
     assert torch.equal(c.v[at, :, 15].float(), (x[0].float() / scale).to(stored).float()) and err.item() == 0
+
+
+@pytest.mark.parametrize("spans", ["decode", "drafts", "chunk_cached", "mixed"])
+@pytest.mark.parametrize("stored,k_scale,scale", [(E4, 1e-20, 1e-30), (BF, None, 2.0 ** -149), (BF, None, 1e-30),
+                                                  (E4, 1e-38, 1.0), (E4, 1e30, 1e20), (BF, None, 3e38)])
+def test_scales_at_the_ends_of_fp32(px, spans, stored, k_scale, scale):
+    """Products far below 1: every key that is seen weighs the same.  Past the other end
+    only queries of zeros have scores that are numbers."""
+    n, total = SPANS[spans]
+    b = dict(batch(px, 62, n, total, 8, 2, 64, 16, stored), scale=scale)
+    if k_scale is not None:
+        b["cache"].k_scale.fill_(k_scale)
+    if scale > 1:
+        b["q"].zero_()
+    got = attend(px, b)
+    assert got[2] == 0
+    check_attention(got, reference(b), 64)
