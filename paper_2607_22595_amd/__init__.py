@@ -230,8 +230,8 @@ _kv_append = _native(
     "k /k v /v @A T req pos rope cache err T_valid stream")
 _paged_attention = _native(
     "xmix_paged_attention_valid",
-    "q:bf16~[T,n,D] cu:i32{C} kv_len:i32[R] cache:struct(Cache) R:dim C:dim D:dim scale:float window:int "
-    "max_q:int out:bf16~[T,n,D] lse?:f32[n,T] err?:i32 ws?:* T_valid?:i32 stream:here",
+    "q:bf16~[T,n,D] cu:i32{C} kv_len:i32[R] cache:struct(Cache) R:dim C:dim D:dim scale:float window:int32 "
+    "max_q:int32 out:bf16~[T,n,D] lse?:f32[n,T] err?:i32 ws?:* T_valid?:i32 stream:here",
     "q /q n T cu kv_len cache scale window max_q out /out lse err ws %ws T_valid stream")
 _graph_launch = _native("xmix_graph_launch", "graph:int stream:stream", "graph stream")
 

@@ -23,14 +23,15 @@
 //   name:bits(n)      a sequence of ints (at most 32 pass); n is bound to its length
 //   name?:struct(S)   the same, or None (a null pointer)
 //   name:int          an int
+//   name:int32        one of 32 bits
 //   name:float        a float
-//   name:dim          an int that the dim of this name is bound to
+//   name:dim          an int (of 32 bits) that the dim of this name is bound to
 //   name:stream       None (the current stream), a torch stream or a handle
 //                     (anything that int() takes)
 //   name:here         the same, and every tensor lives on the current device
 // C arguments: an argument's name, a bound dim, @L (the type code of letter L),
 // #name (the element count of a tensor), %name (its bytes, 0 for None), /name
-// (the distance of its rows in elements).  Floats stand among them in the order
+// (the distance of its rows in elements).  A dim that is passed on has 32 bits.  Floats stand among them in the order
 // of the Python arguments.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -61,6 +62,7 @@ struct Arg {
     int letter = 0;
     bool tail = false, count = false, shaped = false;
     bool rows = false;          // TENSOR: a row distance of its own
+    bool narrow = false;        // INT: of 32 bits
     bool here = false;          // STREAM: tensors of the current device only
     int cut = -1;               // the dim with a ^
     std::vector<int64_t> dims;  // >= 0: a number; -1: any; <= -2: name -2 - v
@@ -248,6 +250,9 @@ PyObject* call(PyObject* self, PyObject* const* argv, size_t nargsf, PyObject* k
             case INT: {
                 const long long v = PyLong_AsLongLong(o);
                 if (v == -1 && PyErr_Occurred()) return nullptr;
+                if (a.narrow && (v < INT32_MIN || v > INT32_MAX))
+                    return PyErr_Format(PyExc_OverflowError, "%s: %s: an int of 32 bits is needed",
+                                        f->name->c_str(), a.name.c_str());
                 value[i] = static_cast<uint64_t>(v);
                 if (a.bind >= 0 && !bind(dims, a.bind, v)) return fail(f, a, "wrong size");
                 break;
@@ -304,7 +309,12 @@ PyObject* call(PyObject* self, PyObject* const* argv, size_t nargsf, PyObject* k
         const Out& o = (*f->outs)[i];
         switch (o.what) {
             case Out::ARG: c[i] = value[o.i]; break;
-            case Out::DIM: c[i] = static_cast<uint64_t>(dims[o.i] < 0 ? 0 : dims[o.i]); break;
+            case Out::DIM:
+                if (dims[o.i] > INT32_MAX)
+                    return PyErr_Format(PyExc_OverflowError, "%s: a size of more than 31 bits",
+                                        f->name->c_str());
+                c[i] = static_cast<uint64_t>(dims[o.i] < 0 ? 0 : dims[o.i]);
+                break;
             case Out::TYPE:
                 c[i] = letters[o.i] == static_cast<int>(at::kBFloat16) ? 1u : 0u;
                 break;
@@ -371,8 +381,9 @@ struct Parser {
             a->kind = STRUCT;
             a->type = reinterpret_cast<PyTypeObject*>(type);
             if (rt) a->bind = dim("T");
-        } else if (t == "int" || t == "dim") {
+        } else if (t == "int" || t == "int32" || t == "dim") {
             a->kind = INT;
+            a->narrow = t != "int";
             if (t == "dim") a->bind = dim(a->name);
         } else if (t == "float") {
             a->kind = FLOAT;

@@ -70,3 +70,14 @@ def test_scales_at_the_ends_of_fp32(px, spans, stored, k_scale, scale):
     got = attend(px, b)
     assert got[2] == 0
     check_attention(got, reference(b), 64)
+
+
+@pytest.mark.parametrize("kw", [dict(window=2 ** 32 + 5), dict(window=2 ** 31), dict(max_q=2 ** 32 + 2)])
+def test_a_window_and_a_bound_of_more_than_32_bits(px, kw):
+    """A window of 2^32 + 5 keys is not one of 5."""
+    b = batch(px, 63, [1, 2], [40, 50], 4, 2, 64, 16)
+    ws = torch.zeros(px.paged_attention_workspace(3, 4, 2, b["cache"]), dtype=torch.uint8, device="cuda")
+    args = dict(dict(scale=0.1, window=0, max_q=2), **kw)
+    with pytest.raises(OverflowError):
+        px.xmix_paged_attention(b["q"], i32(b["cu"]), i32(b["kv_len"]), b["cache"], out=torch.zeros_like(b["q"]),
+                                lse_out=None, err_word=word(), ws=ws, **args)
