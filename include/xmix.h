@@ -683,12 +683,12 @@ xmix_status xmix_kv_append(const void *k, int64_t k_stride, const void *v, int64
  * [0, n_pages) with a key that some token sees sets XMIX_ERR_KV_PAGE and its keys
  * are left out; entries of pages wholly behind the window may hold anything.
  * Requires head_dim 64, 128 or 256, n_q % n_kv == 0, scale > 0 and finite,
- * window >= 0, 1 <= max_q, R_max <= 4096.
+ * window >= 0, 1 <= max_q, R_max <= 4096, T_max * (n_q / n_kv) < 2^31 - 128.
  * ws: 16-byte aligned device workspace of xmix_paged_attention_workspace
  * bytes; nothing in it has to start at zero, and nothing is kept from call to
  * call.  Calls that overlap in time need workspaces of their own.
  * Errors: XMIX_E_INVAL (null pointer, size, stride or alignment),
- * XMIX_E_UNSUPPORTED (head_dim, R_max), XMIX_E_WORKSPACE. */
+ * XMIX_E_UNSUPPORTED (head_dim, R_max, T_max), XMIX_E_WORKSPACE. */
 size_t xmix_paged_attention_workspace(int32_t T_max, int32_t n_q, int32_t max_q,
                                       const xmix_kv_cache *cache);
 xmix_status xmix_paged_attention(const uint16_t *q, int64_t q_stride, int32_t n_q, int32_t T_max,

@@ -628,8 +628,10 @@ bool cache_ok(const xmix_kv_cache* c, KvCacheIn* out) {
 bool attend_heads_ok(int32_t n_q, int32_t max_q, const KvCacheIn& c) {
     return n_q >= 1 && n_q % c.n_kv == 0 && max_q >= 1;
 }
-bool attend_supported(const KvCacheIn& c) {
-    return (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256) && c.R_max <= 4096;
+// The rows of one key head are counted in 32 bits, up to the end of a tile of them.
+bool attend_supported(int32_t T_max, int32_t n_q, const KvCacheIn& c) {
+    return (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256) && c.R_max <= 4096 &&
+           static_cast<int64_t>(T_max) * (n_q / c.n_kv) <= INT32_MAX - 128;
 }
 
 }  // namespace
@@ -683,7 +685,7 @@ size_t xmix_paged_attention_workspace(int32_t T_max, int32_t n_q, int32_t max_q,
                                       const xmix_kv_cache* cache) {
     KvCacheIn c;
     if (T_max < 1 || !cache_ok(cache, &c) || !attend_heads_ok(n_q, max_q, c) ||
-        !attend_supported(c))
+        !attend_supported(T_max, n_q, c))
         return 0;
     return attend_workspace(n_q, max_q, c);
 }
@@ -700,7 +702,7 @@ xmix_status xmix_paged_attention_valid(const uint16_t* q, int64_t q_stride, int3
         !rows_ok(q, q_stride, n_q, c.head_dim, 2, false) ||
         !rows_ok(out, out_stride, n_q, c.head_dim, 2, true))
         return XMIX_E_INVAL;
-    if (!attend_supported(c)) return XMIX_E_UNSUPPORTED;
+    if (!attend_supported(T_max, n_q, c)) return XMIX_E_UNSUPPORTED;
     const size_t need = attend_workspace(n_q, max_q, c);
     if (need && (!ws || !aligned16(ws) || ws_bytes < need)) return XMIX_E_WORKSPACE;
     AttendIn in;
