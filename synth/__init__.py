@@ -404,8 +404,15 @@ def with_attention(wl, n_q, n_kv, ctx_lo=0, ctx_hi=64, page_size=16, rot_dim=Non
     if hd * n_q != wl.d or wl.dtype != "bf16":
         raise ValueError("attention needs a bf16 activation of n_q whole heads")
     cfg = f"{wl.name}/attention"
-    if wl.cu_seqlens is None:  # one token per request, in order
-        wl.cu_seqlens = np.minimum(np.arange(R + 1), wl.T_valid).astype(np.int32)
+    cu = wl.cu_seqlens
+    if cu is None:  # one token per request, in order
+        cu = np.minimum(np.arange(R + 1), wl.T_valid).astype(np.int32)
+    own = np.full(T, -1)
+    own[:cu[-1]] = np.repeat(np.arange(R), np.diff(cu))
+    live = (np.arange(T) < wl.T_valid) & (wl.req >= 0)
+    if (wl.req != own)[live].any():
+        raise ValueError("attention needs each request's tokens in its span of rows")
+    wl.cu_seqlens = cu
     wl.ctx = randint(f"{cfg}/ctx", R, ctx_lo, ctx_hi, seed).astype(np.int32)
     count = -(-(wl.ctx + np.diff(wl.cu_seqlens)) // page_size)
     order = permutation(f"{cfg}/pages", int(count.sum()) + 2, seed)
