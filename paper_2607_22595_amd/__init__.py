@@ -221,17 +221,17 @@ _encode_topk_ring = _native(
 _qk_norm_rope = _native(
     "xmix_qk_norm_rope",
     "q:A~[T,n,D] k?:A~[T,m,D] pos:i32[T] q_w?:A[D] k_w?:A[D] eps:float rope?:struct(Rope) "
-    "q_out:A~[T,n,D] k_out?:A~[T,m,D] T_valid?:i32 stream:here",
+    "q_out:A~[T,n,D] k_out?:A~[T,m,D] T_valid?:i32{1} stream:here",
     "q /q n k /k m @A D T pos q_w k_w eps rope q_out /q_out k_out /k_out T_valid stream")
 _kv_append = _native(
     "xmix_kv_append",
     "k:A~[T,n,D] v:A~[T,n,D] req:i32[T] pos:i32[T] rope?:struct(Rope) cache:struct(Cache) n:dim "
-    "D:dim err?:i32 T_valid?:i32 stream:here",
+    "D:dim err?:i32 T_valid?:i32{1} stream:here",
     "k /k v /v @A T req pos rope cache err T_valid stream")
 _paged_attention = _native(
     "xmix_paged_attention_valid",
     "q:bf16~[T,n,D] cu:i32{C} kv_len:i32[R] cache:struct(Cache) R:dim C:dim D:dim scale:float window:int32 "
-    "max_q:int32 out:bf16~[T,n,D] lse?:f32[n,T] err?:i32 ws?:* T_valid?:i32 stream:here",
+    "max_q:int32 out:bf16~[T,n,D] lse?:f32[n,T] err?:i32 ws?:* T_valid?:i32{1} stream:here",
     "q /q n T cu kv_len cache scale window max_q out /out lse err ws %ws T_valid stream")
 _graph_launch = _native("xmix_graph_launch", "graph:int stream:stream", "graph stream")
 

@@ -81,3 +81,23 @@ def test_a_window_and_a_bound_of_more_than_32_bits(px, kw):
     with pytest.raises(OverflowError):
         px.xmix_paged_attention(b["q"], i32(b["cu"]), i32(b["kv_len"]), b["cache"], out=torch.zeros_like(b["q"]),
                                 lse_out=None, err_word=word(), ws=ws, **args)
+
+
+@pytest.mark.parametrize("count", [0, 2])
+def test_a_count_of_valid_tokens_is_one_number(px, count):
+    """An empty tensor has no address: it would stand for every row."""
+    b = batch(px, 64, [1, 2], [40, 50], 4, 2, 64, 16)
+    c, live = b["cache"], torch.ones(count, dtype=torch.int32, device="cuda")
+    x = torch.zeros(3, 2, 64, dtype=BF, device="cuda")
+    out = torch.full_like(b["q"], 9.0)
+    ws = torch.zeros(px.paged_attention_workspace(3, 4, 2, c), dtype=torch.uint8, device="cuda")
+    before = c.k.clone()
+    with pytest.raises(AssertionError, match="wrong size"):
+        px.xmix_qk_norm_rope(b["q"], None, i32([0, 1, 2]), None, None, 0.0, None, out, None, T_valid=live)
+    with pytest.raises(AssertionError, match="wrong size"):
+        px.xmix_kv_append(x, x, i32([0, 1, 1]), i32([0, 1, 2]), None, c, word(), T_valid=live)
+    with pytest.raises(AssertionError, match="wrong size"):
+        px.xmix_paged_attention(b["q"], i32(b["cu"]), i32(b["kv_len"]), c, 0.1, 0, 2, out, None, word(), ws,
+                                T_valid=live)
+    torch.cuda.synchronize()
+    assert bool((out == 9).all()) and torch.equal(c.k, before)
