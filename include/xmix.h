@@ -667,7 +667,8 @@ xmix_status xmix_kv_append(const void *k, int64_t k_stride, const void *v, int64
  *   out = sum_j exp(s_j - lse) v_j
  * with q . k_j in exact bf16 products summed in fp32, the statistics in fp32,
  * exp(s_j - max) rounded to bf16 where it multiplies v_j, and one rounding of
- * out.  A masked key has no effect whatever its slots hold (NaN, infinities).
+ * out.  max is a running one that leaves terms of up to 2^8 |v_j|, whose sum has to
+ * stay in fp32's range: values up to 2^88 in size do, whatever their number.  A masked key has no effect whatever its slots hold (NaN, infinities).
  * A token without a key (p < 0) gets zeros and lse = -infinity.
  * One call serves any mix of spans: one token per request (decode), a few
  * (drafted tokens), chunks of a prompt.  The keys of a span are shared out in

@@ -91,10 +91,22 @@ struct Deal {
     int32_t queue_from;             // queued, in launches of so many places a workgroup
 };
 // A block of a tile takes half as long again as one of a row unit (1.4 us and 0.9 us
-// at head_dim 64, two workgroups on a CU), a unit's own cost is 6 to 8 us; sixteen
-// prompts took 145 us with 9 places for it, 150 with 12 and 148 with 15.  A launch of
-// row units alone takes 643 us with 4 (256 requests of up to 8192 keys), 640 with 2,
-// 652 with 8; one request of 1024 keys 16.0, 18.7 and 16.1.
+// at head_dim 64, two workgroups on a CU), a unit's own cost is 6 to 8 us.  The numbers
+// were found at head_dim 64 and 128 in bf16; us with others, at every width and type:
+//   extra of a row unit (256 requests of up to 8192 keys)      2     4     8
+//     head_dim 64, bf16 and e4m3                         344 186  335 182  338 175
+//     128, bf16 and e4m3 (24 requests of up to 65536)    640 321  642 320  667 320
+//     256, bf16 and e4m3                                 629 385  628 366  642 368
+//     128, bf16, one request of 1024 keys                  18.0     15.5    15.6
+//   extra of a tile                                            6     9    14
+//     sixteen prompts, 128, bf16 and e4m3                139 136  138 136  138 137
+//     the same at 256                                    109 108  109 108  108 108
+//     95 single tokens and a chunk, 64, bf16 and e4m3    128 132  127 133  127 134
+//     the same at 256, bf16                                 258     246     256
+//   few_step (the single tokens and the chunk)                 1     2     4
+//     64, bf16 and e4m3                                  129 120  127 133  156 127
+//     256, bf16                                             333     246     295
+// One set serves them within 5 %, but for single tokens among tiles in e4m3.
 // Of a long launch of tiles the short units that lead each request (the first tokens of
 // a prompt) are left for whoever ends its range first: sixteen prompts 153 -> 142 us,
 // one of 2000 tokens 138 -> 119.  A short launch would pay for the queue's round trips
@@ -209,8 +221,9 @@ __device__ __forceinline__ int64_t wave_sum64(int64_t v) {
 // one may (MANY), a wave for each that does and a wave a range, with as many
 // workgroups as there are ranges for (all find the same prefix): walking over 64 tiles
 // a thread took 25 us on the one CU.  Chains of round trips and of 64-bit divisions
-// are what it costs: 8 us with the spans in LDS and short divisions (11 before) in a
-// batch of 96 requests, 3 us for one request.
+// are what it costs (spans in LDS and short divisions saved 3 us of 11 in a batch of 96
+// requests, before the queue).  In a trace it takes 5 us for one request, 8 for 256 of
+// one token, and 12 to 13 in the form for many tiles, for 96 requests, 16 or one.
 //
 // A range that would begin inside a short tile unit (up to `whole` blocks) begins at
 // the nearer end of it instead: its parts would take their way through memory, 64 KB
@@ -613,8 +626,11 @@ __device__ __forceinline__ float score_scale(float scale, float k_scale) {
     const float c = scale * k_scale * kLog2e;
     return c == 0.0f ? 0x1p-149f : c == INFINITY ? 0x1.fffffep127f : c;
 }
-// Weights to bf16, nearest even: 2^-9 of each on average, which the sum over many
-// keys averages out; the sum of the weights keeps them in fp32.
+// Weights to bf16, nearest even, at most 2^-8 of each: the matrix instructions take both
+// operands in one type, and a second one for what is cut off would be half as many again.
+// The sum over many keys averages it out: the result's relative error (its norm) is 0.0020
+// to 0.0023, of which its own rounding alone makes 0.0017.  The sum of the weights keeps
+// them in fp32.
 __device__ __forceinline__ uint32_t weights2(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{a, b}, bf16x2_t));
 }
@@ -835,13 +851,17 @@ struct UnitLds {
 // product; K and V of a block come by copies into LDS, the block behind it while this
 // one is multiplied, and every operand read from there serves 32 rows.
 //
-// The matrix units and the device's power bound it: 4096 tokens over 32768 keys, 32
-// heads of 128, run at 930 to 990 TFLOP/s (2.1 to 2.2 ms; 53 % of the cycles in matrix
-// instructions, the library's plain product reaches 1249).  With few blocks a unit
-// its start does, the chain from page id to copy to first product: units of one block
-// take 9 us, of eight 18 (sixteen prompts of up to 1024 tokens: 143 us, 485 TFLOP/s).
+// The matrix units bound it: 4096 tokens over 32768 keys, 32 heads of 128, run at 930 to
+// 960 TFLOP/s (2.15 to 2.22 ms, 52 % of the cycles in matrix instructions, at a clock of
+// about 1.8 GHz; the library's plain product reaches 1249).  In e4m3, with a conversion
+// of every operand and half the bytes, the same takes 2.1 to 2.2 ms; at head_dim 256, one
+// workgroup on a CU and some registers spilled, 2.5.  With few blocks a unit its start
+// bounds it, the chain from page id to copy to first product: sixteen prompts of up to
+// 1024 tokens take 138 to 145 us, 480 to 500 TFLOP/s; with time stamps in the kernel,
+// which make it 25 % slower, units of one block take 14 us there and of eight 25 to 28.
 // The next unit's first copies issued before this one's rows are stored did not help
-// (147 to 159 us), the CU's second workgroup being at work meanwhile.
+// (147 us before the queue, 147 to 159 so), the CU's second workgroup being at work
+// meanwhile.
 template <int HD, bool E4M3>
 __device__ __forceinline__ void tile_unit(const AttendIn& in, const KvCacheIn& cache, const AttendWs& ws,
                                           const WorkRange& st, const Span& s, const Blocks& bl,
@@ -1133,9 +1153,10 @@ struct RowStep {
 //
 // Memory bounds it: 256 requests of up to 8192 keys, heads of 128, read 4.1 GB (what
 // they hold, by the counters too) in 643 us, 6.4 TB/s of the 7.0 that a plain read
-// reaches; in e4m3 2.0 GB take 320 us, 6.3 TB/s; with 32 rows a unit (five tokens a
-// request, a window of 4096) 0.84 GB take 177 to 189 us, where a unit's start, its
-// parts and their join are 17 to 20 us of about 130.
+// reaches; in e4m3 2.0 GB take 320 us, 6.3 TB/s; at head_dim 256 4.1 GB take 630 us, and
+// 2.0 GB of e4m3 366; at 64 2.0 GB take 335 and 1.0 GB of e4m3 182.  With 32 rows a unit
+// (five tokens a request, a window of 4096) 0.84 GB take 174 to 180 us, where a unit's
+// start, its parts and their join are 16 to 20 of about 130.
 template <int HD, bool E4M3, int NB, int SLOT>
 __device__ __forceinline__ void row_unit(const AttendIn& in, const KvCacheIn& cache, const AttendWs& ws,
                                          const WorkRange& st, const Span& s, const Blocks& bl,
@@ -1548,8 +1569,10 @@ int32_t unit_rows(int32_t n_q, int32_t max_q, const KvCacheIn& c) {
     const int64_t rows = static_cast<int64_t>(max_q) * (n_q / c.n_kv);
     return rows <= 16 ? 16 : rows <= 32 && c.head_dim < 256 ? 32 : kTileRows;
 }
-// Workgroups of a launch: as many as the chip holds at a time (two on a CU where
-// their registers allow it).
+// Workgroups of a launch: as many as the chip holds at a time, two on a CU where their
+// registers and LDS allow it.  At head_dim 256 they do not, and twice as many, one round
+// behind the other, take 650 us for 628 (256 single tokens), 124 for 109 (prompts), 318
+// for 246 (single tokens and a chunk).
 int32_t workgroups(int32_t rows, const KvCacheIn& c) {
     return c.head_dim > 128 ? 256 : 512;
 }

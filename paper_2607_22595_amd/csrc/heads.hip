@@ -168,9 +168,10 @@ __device__ __forceinline__ uint32_t pack4_e4m3(const float* x) {
 
 // The threads that a token's heads need, a workgroup's at most: their lane groups take
 // the token's key heads, rotated, and its value heads in turn, and store each into the token's slot.  Sixteen prompts'
-// 9982 tokens of 8 heads of 128 into e4m3 pages: 15.9 us for 61 MB, 3.9 TB/s (17.0
-// with a full division a value, 19.3 with a workgroup for each token and half of its
-// threads idle); 256 tokens into bf16 pages: 3.4 us, a chain of three round trips.
+// 9982 tokens of 8 heads of 128 into e4m3 pages: 14.6 us for 61 MB, 4.2 TB/s (in a trace
+// 15.3; 15.9 when it was 17.0 with a full division a value, 19.3 with a workgroup for each
+// token and half of its threads idle); 256 tokens into bf16 pages: 3.4 us, a chain of
+// three round trips.
 template <bool BF16, bool E4M3>
 __global__ void __launch_bounds__(kHeadThreads)
 kv_append_kernel(const void* __restrict__ k, int64_t k_stride, const void* __restrict__ v,
